@@ -65,7 +65,9 @@ enum {
   SKIPKV_DEV_TOO_MANY_TOK = 8,  /* skipkv_select_tokens: a sequence is longer than SKIPKV_MAX_TOKENS_TOKEN_SELECT */
   SKIPKV_DEV_BAD_BLOCK_TABLE = 16, /* paged cache: a block id outside [0, n_blocks); that sequence's K/V are left untouched */
   SKIPKV_DEV_BAD_BUDGET = 32,   /* a device budget below the protected window, negative, or too large for kept_stride */
-  SKIPKV_DEV_BAD_SCORES = 64    /* selection: a candidate sentence's score is NaN                 */
+  SKIPKV_DEV_BAD_SCORES = 64,   /* selection: a candidate sentence's score is NaN                 */
+  SKIPKV_DEV_BAD_LENGTHS = 128, /* 8-bit cache, pages: a length, row range or query offset that does not fit */
+  SKIPKV_DEV_OUT_OF_BLOCKS = 256 /* skipkv_pages_update: too few free blocks, or table rows too short */
 };
 /*
  * A head (layer, KV head, sequence) that one of these bits concerns is never compacted from
@@ -512,6 +514,138 @@ int skipkv_score_ranges_paged(const skipkv_cache *cache, const skipkv_ranges *ra
 int skipkv_token_redundancy_ranges_paged(const skipkv_cache *cache, const skipkv_ranges *ranges, const skipkv_paging *paging,
                                          float *tok_redundancy, int32_t *dev_status, void *ws, size_t ws_bytes,
                                          void *stream);
+
+/*
+ * Block tables of a paged cache on the GPU: what the decode loop does around the step, whose compaction
+ * leaves blocks beyond the new lengths (release) and whose next tokens need further ones (growth).
+ */
+typedef struct skipkv_pages {
+  int32_t *block_table; /* device [batch, table_stride]; the first n_held[b] entries of row b are sequence b's blocks */
+  int32_t *n_held;      /* device [batch]                                                      */
+  int32_t *free_list;   /* device [n_blocks]: a stack of free block ids, its top at n_free - 1    */
+  int32_t *n_free;      /* device [1]                                                          */
+  int32_t batch;        /* at most SKIPKV_MAX_PAGES_BATCH                                        */
+  int32_t table_stride;
+  int32_t block_size;   /* token slots per block, >= 1                                          */
+  int32_t n_blocks;
+} skipkv_pages;
+#define SKIPKV_MAX_PAGES_BATCH 4096
+
+/*
+ * Brings every sequence to need_b = ceil((max_r len[r, b] + n_new_b) / block_size) blocks, in place:
+ *   release   sequences with n_held > need push entries need .. n_held-1 of their row onto the free
+ *             stack, in order of the sequence, then of the entry;
+ *   growth    sequences with n_held < need take blocks off the top of the stack, in the same order.
+ *             First come, first served: from the first sequence on for which too few blocks are left, none grows
+ *             (SKIPKV_DEV_OUT_OF_BLOCKS; n_held says which).  A sequence with need > table_stride stays as it
+ *             is and counts for nothing (same bit).
+ * Table entries at and beyond n_held and stack entries at and beyond n_free keep what they held.
+ * slot_map[r * total_new + i], for the new token i = new_off[b] .. new_off[b+1]-1 of sequence b, is the slot
+ *   block * block_size + (slot in the block) of position len[r, b] + i - new_off[b], where its K and V rows
+ *   go; -1 where the sequence does not hold the block.
+ * len       device [n_rows, batch]: lengths before the new tokens; n_rows = 1 for lengths shared by all
+ *           heads, n_layers * n_kv_heads for skipkv_ranges.len.
+ * new_off   device [batch + 1] CSR of the new tokens, or NULL (none); total_new = host copy of new_off[batch].
+ * slot_map  device out [n_rows, total_new] int32, or NULL.
+ * A negative length or count leaves that sequence as it is (SKIPKV_DEV_BAD_LENGTHS, slots -1); n_held or n_free out
+ * of range, or more blocks given back than the stack has room for, leave everything as it is
+ * (SKIPKV_DEV_BAD_BLOCK_TABLE, all slots -1).
+ * dev_status  device int32, OR-ed into; may be NULL.
+ * ws        device scratch of at least skipkv_pages_workspace_bytes, 256-byte aligned.
+ */
+int skipkv_pages_workspace_bytes(const skipkv_pages *pages, size_t *out_bytes);
+int skipkv_pages_update(const skipkv_pages *pages, const int32_t *len, int32_t n_rows, const int32_t *new_off,
+                        int32_t total_new, int32_t *slot_map, int32_t *dev_status, void *ws, size_t ws_bytes,
+                        void *stream);
+
+/*
+ * KV cache held in 8 bits: pools of blocks as in skipkv_paging, whose elements are e4m3 codes (OCP:
+ * largest value 448, no infinities, 0x7F and 0xFF are NaN) with one scale per layer, KV head and
+ * block for K and one for V.  A scale is a byte e in 1 .. 247 (what any fp32 row needs at most) that stands for 2^(e - 127),
+ * so element = code * 2^(e - 127).
+ * Scales being powers of two, a stored value is a bf16 number (but for values below 2^-133), and it stays
+ * the same number when it is loaded, moved to another block and stored again, unless it falls
+ * among the subnormals there (below 2^-6 of the new scale).
+ * Strides are in elements (= bytes) and multiples of 16; element (l, h, block p, slot s, d) at
+ * l * stride_layer + h * stride_head + p * stride_block + s * stride_tok + d.  Lengths are per head like skipkv_ranges.len.
+ */
+typedef struct skipkv_quant_cache {
+  void *k;               /* device pools, 16-byte aligned                                      */
+  void *v;
+  uint8_t *k_exp;        /* device [n_layers, n_kv_heads, n_blocks] scale bytes                   */
+  uint8_t *v_exp;
+  int64_t stride_layer;
+  int64_t stride_head;
+  int64_t stride_block;  /* >= block_size * stride_tok                                           */
+  int64_t stride_tok;    /* >= head_dim                                                        */
+  int32_t n_layers;
+  int32_t n_kv_heads;
+  int32_t head_dim;      /* must be 128                                                        */
+  int32_t batch;         /* at most 65535                                                      */
+  int32_t block_size;    /* 16, 32, 64 or 128                                                  */
+  int32_t n_blocks;
+  int32_t table_stride;
+  const int32_t *block_table; /* device [batch, table_stride]                                   */
+} skipkv_quant_cache;
+
+/*
+ * Rows of a dense cache to and from the 8-bit one.  rows describes the dense side: k, v, strides, dtype,
+ * n_layers, n_kv_heads, head_dim, batch, total_tokens and seq_off are used; its layer l is layer
+ * first_layer + l of qc.  For every head (l, h, b), positions begin .. end-1 of the sequence belong to
+ * rows seq_off[b] .. seq_off[b] + end - begin - 1 of rows.
+ *   begin  device [rows->n_layers, n_kv_heads, batch], or NULL: 0
+ *   end    device, same shape, or NULL: begin + seq_off[b+1] - seq_off[b]
+ * So a compacted cache goes in with begin = NULL, end = new_len; new tokens, packed by seq_off, with begin = the lengths
+ * before them and end = NULL; and the cache comes back for skipkv_step_ranges with begin = NULL, end = len.
+ * skipkv_quant_store: per block and head, the scale is the least 2^e (e - 127 as above) with
+ *   448 * 2^e >= the largest finite magnitude stored; values are rounded to nearest, ties to even; infinities and NaN become
+ *   NaN.  A block that holds positions before begin keeps its scale if that is the larger one, else those are
+ *   rounded again to the new scale.  Slots at and beyond end are not written.
+ * skipkv_quant_load: code * 2^(e - 127), rounded once to the dtype of rows; other rows are not written.
+ * A range with begin < 0, end < begin, end > table_stride * block_size or longer than seq_off[b+1] - seq_off[b] is skipped
+ * (SKIPKV_DEV_BAD_LENGTHS); positions in a block whose id is outside [0, n_blocks) are skipped
+ * (SKIPKV_DEV_BAD_BLOCK_TABLE).  Blocks that are stored to must belong to one sequence only.
+ * dev_status  device int32, OR-ed into; may be NULL.
+ */
+int skipkv_quant_store(const skipkv_quant_cache *qc, const skipkv_cache *rows, int32_t first_layer,
+                       const int32_t *begin, const int32_t *end, int32_t *dev_status, void *stream);
+int skipkv_quant_load(const skipkv_quant_cache *qc, const skipkv_cache *rows, int32_t first_layer,
+                      const int32_t *begin, const int32_t *end, int32_t *dev_status, void *stream);
+
+/* The query tokens of an attention call: the last m_b = q_off[b+1] - q_off[b] tokens of sequence b. */
+typedef struct skipkv_queries {
+  const void *q;           /* device; head i of token t at q + t * q_stride_tok + i * q_stride_head, 16-byte aligned */
+  void *out;               /* device, likewise with out_stride_*; must not overlap q              */
+  float *lse;              /* device [total_q, n_q_heads], or NULL                               */
+  int64_t q_stride_tok, q_stride_head;     /* elements, multiples of 8                            */
+  int64_t out_stride_tok, out_stride_head; /* elements, multiples of 8, >= head_dim                 */
+  int32_t dtype;           /* skipkv_dtype of q and out                                          */
+  int32_t n_q_heads;       /* a multiple of the KV heads, at most SKIPKV_MAX_GROUP times as many    */
+  int32_t total_q;         /* host copy of q_off[batch]                                          */
+  int32_t max_q;           /* host upper bound on any m_b                                        */
+  int32_t max_len;         /* host upper bound on any length                                     */
+  float scale;             /* of the logits, usually 1 / sqrt(head_dim)                          */
+  const int32_t *q_off;    /* device [batch + 1]                                                 */
+} skipkv_queries;
+
+/*
+ * Attention of one layer over the 8-bit cache: with N = len[h, b], query token j = 0 .. m_b-1 of sequence b
+ * is at position N - m_b + j and sees keys t <= N - m_b + j; query head i uses KV head i / n:
+ *   out = sum_t softmax_t(scale * q.k_t) v_t,   lse = log sum_t exp(scale * q.k_t)  (natural logarithm).
+ * A query that sees no key (N < m_b: its position is negative) gets out = 0, lse = -inf.  Slots beyond N and keys that
+ * a query does not see have no influence on it, whatever they hold.
+ * len   device [n_kv_heads, batch]: this layer's lengths, the query tokens included.
+ * The result does not depend on max_len and max_q but for the order of additions.  A length that is negative, above
+ * max_len or above table_stride * block_size (SKIPKV_DEV_BAD_LENGTHS), or a block id outside [0, n_blocks) among a head's
+ * blocks (SKIPKV_DEV_BAD_BLOCK_TABLE), makes the rows concerned NaN; a sequence whose q_off entries
+ * descend, leave [0, total_q] or are more than max_q apart gets no output (SKIPKV_DEV_BAD_LENGTHS).
+ * dev_status  device int32, OR-ed into; may be NULL.
+ * ws    device scratch of at least skipkv_quant_attend_workspace_bytes (0 is possible: then ws may be
+ *       NULL), 256-byte aligned.
+ */
+int skipkv_quant_attend_workspace_bytes(const skipkv_quant_cache *qc, const skipkv_queries *queries, size_t *out_bytes);
+int skipkv_quant_attend(const skipkv_quant_cache *qc, int32_t layer, const skipkv_queries *queries, const int32_t *len,
+                        int32_t *dev_status, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Steering injection (Sec. 4.2): hidden[b, :] <- hidden[b, :] + coef_b * vec for every row b

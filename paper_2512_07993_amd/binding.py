@@ -17,6 +17,7 @@ import torch
 F32, BF16 = 0, 1
 OK, EINVAL, EBUDGET, ECAPACITY, EWORKSPACE, EHIP = 0, -1, -2, -3, -4, -5
 DEV_BAD_OFFSETS, DEV_TOO_MANY_SENT, DEV_TIMEOUT, DEV_TOO_MANY_TOK, DEV_BAD_BLOCK_TABLE, DEV_BAD_BUDGET, DEV_BAD_SCORES = 1, 2, 4, 8, 16, 32, 64
+DEV_BAD_LENGTHS, DEV_OUT_OF_BLOCKS = 128, 256
 FLAG_FORCE_TWO_PASS = 1
 PROFILE_SLOTS = 16
 
@@ -42,6 +43,29 @@ class CRanges(C.Structure):
 class CPaging(C.Structure):
     _fields_ = [("block_table", C.c_void_p), ("table_stride", C.c_int32), ("block_size", C.c_int32),
                 ("n_blocks", C.c_int32), ("stride_block", C.c_int64)]
+
+
+class CPages(C.Structure):
+    _fields_ = [("block_table", C.c_void_p), ("n_held", C.c_void_p), ("free_list", C.c_void_p), ("n_free", C.c_void_p),
+                ("batch", C.c_int32), ("table_stride", C.c_int32), ("block_size", C.c_int32), ("n_blocks", C.c_int32)]
+
+
+class CQuantCache(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+        ("stride_layer", C.c_int64), ("stride_head", C.c_int64), ("stride_block", C.c_int64), ("stride_tok", C.c_int64),
+        ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("batch", C.c_int32),
+        ("block_size", C.c_int32), ("n_blocks", C.c_int32), ("table_stride", C.c_int32), ("block_table", C.c_void_p),
+    ]
+
+
+class CQueries(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+        ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64), ("out_stride_tok", C.c_int64), ("out_stride_head", C.c_int64),
+        ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("total_q", C.c_int32), ("max_q", C.c_int32), ("max_len", C.c_int32),
+        ("scale", C.c_float), ("q_off", C.c_void_p),
+    ]
 
 
 class CParams(C.Structure):
@@ -103,6 +127,13 @@ def lib() -> C.CDLL:
         L.skipkv_token_redundancy_ranges_paged.argtypes = [cp, rp, gp, vp, vp, vp, sz, vp]
         L.skipkv_ranges_paged_workspace_bytes.argtypes = [cp, gp, pp, C.POINTER(sz)]
         L.skipkv_step_ranges_paged.argtypes = [cp, rp, gp, pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+        sp, qp, np_ = C.POINTER(CPages), C.POINTER(CQuantCache), C.POINTER(CQueries)
+        L.skipkv_pages_workspace_bytes.argtypes = [sp, C.POINTER(sz)]
+        L.skipkv_pages_update.argtypes = [sp, vp, i32, vp, i32, vp, vp, vp, sz, vp]
+        L.skipkv_quant_store.argtypes = [qp, cp, i32, vp, vp, vp, vp]
+        L.skipkv_quant_load.argtypes = [qp, cp, i32, vp, vp, vp, vp]
+        L.skipkv_quant_attend_workspace_bytes.argtypes = [qp, np_, C.POINTER(sz)]
+        L.skipkv_quant_attend.argtypes = [qp, i32, np_, vp, vp, vp, sz, vp]
         L.skipkv_profile_create.argtypes = [C.POINTER(vp)]
         L.skipkv_profile_read.argtypes = [vp, C.POINTER(i32), C.POINTER(C.c_char_p), C.POINTER(fl)]
         L.skipkv_profile_destroy.argtypes = [vp]
@@ -114,6 +145,8 @@ def lib() -> C.CDLL:
                      "skipkv_select_tokens", "skipkv_ranges_workspace_bytes", "skipkv_ranges_append", "skipkv_step_ranges",
                      "skipkv_similarity_workspace_bytes", "skipkv_sentence_similarity", "skipkv_score_shared", "skipkv_steer_strength",
                      "skipkv_paged_workspace_bytes", "skipkv_step_paged",
+                     "skipkv_pages_workspace_bytes", "skipkv_pages_update", "skipkv_quant_store", "skipkv_quant_load",
+                     "skipkv_quant_attend_workspace_bytes", "skipkv_quant_attend",
                      "skipkv_profile_create", "skipkv_profile_read", "skipkv_profile_destroy",
                      "skipkv_version"):
             getattr(L, name).restype = C.c_int
@@ -459,6 +492,103 @@ def skipkv_step_ranges_paged(cache: PagedCache, ranges: Ranges, params: Params, 
                                           _ptr(sent_lambda), _ptr(tok_importance), _ptr(sent_keep), _ptr(kept_idx),
                                           _ptr(new_len), _ptr(new_sent_off), _ptr(new_sent_cnt), kept_stride, _ptr(ws),
                                           ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)))
+
+
+@dataclass
+class Pages:
+    """Python mirror of skipkv_pages: block_table [B, table_stride], n_held [B], free_list [n_blocks] and
+    n_free [1], int32 device tensors that skipkv_pages_update changes in place."""
+    block_table: torch.Tensor
+    n_held: torch.Tensor
+    free_list: torch.Tensor
+    n_free: torch.Tensor
+    block_size: int
+
+    def c(self) -> CPages:
+        bt = self.block_table
+        assert bt.dim() == 2 and bt.shape[0] == self.n_held.numel() and (bt.stride(1) == 1 or bt.shape[1] <= 1)
+        assert all(t.dtype == torch.int32 for t in (bt, self.n_held, self.free_list, self.n_free))
+        assert self.n_held.is_contiguous() and self.free_list.is_contiguous()
+        return CPages(bt.data_ptr(), _ptr(self.n_held), _ptr(self.free_list), _ptr(self.n_free), bt.shape[0], bt.stride(0),
+                      self.block_size, self.free_list.numel())
+
+
+def skipkv_pages_workspace_bytes(pages: Pages) -> int:
+    out = C.c_size_t(0)
+    _check(lib().skipkv_pages_workspace_bytes(C.byref(pages.c()), C.byref(out)))
+    return int(out.value)
+
+
+def skipkv_pages_update(pages: Pages, len, new_off, total_new: int, slot_map, ws, dev_status=None, stream=None) -> None:
+    """len: [n_rows, B] (or [L, Hk, B]: n_rows = L * Hk); new_off: [B + 1] or None; slot_map: [n_rows, total_new] or None."""
+    assert len.is_contiguous() and len.dtype == torch.int32 and len.shape[-1] == pages.n_held.numel()
+    n_rows = len.numel() // max(len.shape[-1], 1) if len.numel() else 1
+    assert slot_map is None or (slot_map.is_contiguous() and slot_map.dtype == torch.int32 and slot_map.numel() == n_rows * total_new)
+    _check(lib().skipkv_pages_update(C.byref(pages.c()), _ptr(len), n_rows, _ptr(new_off), total_new, _ptr(slot_map),
+                                     _ptr(dev_status), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+@dataclass
+class QuantCache:
+    """Python mirror of skipkv_quant_cache for pools laid out [L, blocks, slots, Hk, D] (any strides with D
+    contiguous) of uint8 or float8_e4m3fn, scale bytes [L, Hk, blocks] and a block table [B, table_stride]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_exp: torch.Tensor
+    v_exp: torch.Tensor
+    block_table: torch.Tensor
+
+    def c(self) -> CQuantCache:
+        k, bt = self.k, self.block_table
+        assert k.dim() == 5 and k.element_size() == 1 and k.stride(4) == 1 and self.v.stride() == k.stride() and self.v.shape == k.shape
+        assert self.v.element_size() == 1
+        for e in (self.k_exp, self.v_exp):
+            assert e.dtype == torch.uint8 and e.is_contiguous() and e.shape == (k.shape[0], k.shape[3], k.shape[1])
+        assert bt.dim() == 2 and bt.dtype == torch.int32 and (bt.stride(1) == 1 or bt.shape[1] <= 1)
+        return CQuantCache(_ptr(k), _ptr(self.v), _ptr(self.k_exp), _ptr(self.v_exp), k.stride(0), k.stride(3), k.stride(1),
+                           k.stride(2), k.shape[0], k.shape[3], k.shape[4], bt.shape[0], k.shape[2], k.shape[1], bt.stride(0),
+                           _ptr(bt))
+
+
+@dataclass
+class Queries:
+    """Python mirror of skipkv_queries: q and out [total_q, Hq, D] (any strides with D contiguous), lse [total_q, Hq] fp32 or None."""
+    q: torch.Tensor
+    out: torch.Tensor
+    q_off: torch.Tensor        # int32 device [B+1]
+    max_q: int
+    max_len: int
+    scale: float
+    lse: Optional[torch.Tensor] = None
+
+    def c(self) -> CQueries:
+        q, o = self.q, self.out
+        assert q.dim() == 3 and o.shape == q.shape and o.dtype == q.dtype and q.stride(2) == 1 and o.stride(2) == 1
+        assert self.lse is None or (self.lse.is_contiguous() and self.lse.dtype == torch.float32 and self.lse.shape == q.shape[:2])
+        return CQueries(_ptr(q), _ptr(o), _ptr(self.lse), q.stride(0), q.stride(1), o.stride(0), o.stride(1), dtype_code(q.dtype),
+                        q.shape[1], q.shape[0], self.max_q, self.max_len, self.scale, _ptr(self.q_off))
+
+
+def skipkv_quant_store(qc: QuantCache, rows: Cache, first_layer: int, begin, end, dev_status=None, stream=None) -> None:
+    _check(lib().skipkv_quant_store(C.byref(qc.c()), C.byref(rows.c()), first_layer, _ptr(begin), _ptr(end), _ptr(dev_status),
+                                    _stream(stream)))
+
+
+def skipkv_quant_load(qc: QuantCache, rows: Cache, first_layer: int, begin, end, dev_status=None, stream=None) -> None:
+    _check(lib().skipkv_quant_load(C.byref(qc.c()), C.byref(rows.c()), first_layer, _ptr(begin), _ptr(end), _ptr(dev_status),
+                                   _stream(stream)))
+
+
+def skipkv_quant_attend_workspace_bytes(qc: QuantCache, queries: Queries) -> int:
+    out = C.c_size_t(0)
+    _check(lib().skipkv_quant_attend_workspace_bytes(C.byref(qc.c()), C.byref(queries.c()), C.byref(out)))
+    return int(out.value)
+
+
+def skipkv_quant_attend(qc: QuantCache, layer: int, queries: Queries, len, ws, dev_status=None, stream=None) -> None:
+    assert len.is_contiguous() and len.dtype == torch.int32 and len.shape == (qc.k.shape[3], qc.block_table.shape[0])
+    _check(lib().skipkv_quant_attend(C.byref(qc.c()), layer, C.byref(queries.c()), _ptr(len), _ptr(dev_status), _ptr(ws),
+                                     _nbytes(ws), _stream(stream)))
 
 
 def skipkv_similarity_workspace_bytes(cache: Cache, d_model: int) -> int:

@@ -1239,6 +1239,218 @@ int token_redundancy_paged(const skipkv_cache *cache, const int32_t *len, const 
 }
 }  // namespace
 
+// ---- block tables on the GPU -------------------------------------------------------------------------------
+
+namespace {
+int check_pages(const skipkv_pages *pg) {
+  if (!pg || pg->batch < 0 || pg->table_stride < 0 || pg->block_size < 1 || pg->n_blocks < 1) return SKIPKV_EINVAL;
+  if (pg->batch > SKIPKV_MAX_PAGES_BATCH) return SKIPKV_ECAPACITY;
+  if ((int64_t)pg->n_blocks * pg->block_size > 0x7FFFFFFFll) return SKIPKV_ECAPACITY;  // slots are 32-bit
+  if (pg->batch > 0 && (!pg->n_held || !pg->free_list || !pg->n_free || (!pg->block_table && pg->table_stride > 0))) return SKIPKV_EINVAL;
+  return SKIPKV_OK;
+}
+size_t pages_need_bytes(const skipkv_pages *pg) { return align_up((size_t)pg->batch * 4); }
+}  // namespace
+
+int skipkv_pages_workspace_bytes(const skipkv_pages *pages, size_t *out_bytes) {
+  if (!out_bytes) return SKIPKV_EINVAL;
+  const int rc = check_pages(pages);
+  if (rc) return rc;
+  *out_bytes = pages->batch == 0 ? 0 : pages_need_bytes(pages) + align_up(((size_t)pages->batch + 1) * 4);
+  return SKIPKV_OK;
+}
+
+int skipkv_pages_update(const skipkv_pages *pages, const int32_t *len, int32_t n_rows, const int32_t *new_off,
+                        int32_t total_new, int32_t *slot_map, int32_t *dev_status, void *ws, size_t ws_bytes, void *stream) {
+  size_t need = 0;
+  const int rc = skipkv_pages_workspace_bytes(pages, &need);
+  if (rc) return rc;
+  if (n_rows < 1 || total_new < 0 || (!new_off && total_new > 0)) return SKIPKV_EINVAL;
+  if (pages->batch == 0) return SKIPKV_OK;
+  if (!len) return SKIPKV_EINVAL;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < need) return SKIPKV_EWORKSPACE;
+  PagesArgs a{};
+  a.block_table = pages->block_table;
+  a.n_held = pages->n_held;
+  a.free_list = pages->free_list;
+  a.n_free = pages->n_free;
+  a.batch = pages->batch;
+  a.table_stride = pages->table_stride;
+  a.block_size = pages->block_size;
+  a.n_blocks = pages->n_blocks;
+  a.len = len;
+  a.new_off = new_off;
+  a.n_rows = n_rows;
+  a.total_new = total_new;
+  a.slot_map = total_new > 0 ? slot_map : nullptr;
+  a.dev_status = dev_status;
+  a.need = static_cast<int32_t *>(ws);
+  a.was_held = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + pages_need_bytes(pages));
+  return launch_pages_update(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SKIPKV_OK : SKIPKV_EHIP;
+}
+
+// ---- 8-bit cache -------------------------------------------------------------------------------------------
+
+namespace {
+bool quant_empty(const skipkv_quant_cache *c) { return c->n_layers == 0 || c->n_kv_heads == 0 || c->batch == 0; }
+
+int check_quant(const skipkv_quant_cache *c) {
+  if (!c) return SKIPKV_EINVAL;
+  if (c->head_dim != SKIPKV_HEAD_DIM) return SKIPKV_ECAPACITY;
+  if (c->n_layers < 0 || c->n_kv_heads < 0 || c->batch < 0 || c->table_stride < 0 || c->n_blocks < 1) return SKIPKV_EINVAL;
+  if (c->block_size != 16 && c->block_size != 32 && c->block_size != 64 && c->block_size != 128) return SKIPKV_ECAPACITY;
+  if (quant_empty(c)) return SKIPKV_OK;
+  if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v) || !c->k_exp || !c->v_exp) return SKIPKV_EINVAL;
+  if (!c->block_table && c->table_stride > 0) return SKIPKV_EINVAL;
+  if (c->stride_layer < 0 || c->stride_head < 0 || c->stride_tok < c->head_dim) return SKIPKV_EINVAL;
+  if ((c->stride_layer % 16) || (c->stride_head % 16) || (c->stride_block % 16) || (c->stride_tok % 16)) return SKIPKV_EINVAL;
+  // a block is addressed by 32-bit offsets, positions are 32-bit
+  if (c->stride_tok > (1ll << 31) / 128 - 1 || (int64_t)c->table_stride * c->block_size > 0x7FFFFF00ll) return SKIPKV_ECAPACITY;
+  if (c->batch > 65535 || (int64_t)c->n_layers * c->n_kv_heads > 32767) return SKIPKV_ECAPACITY;
+  if (c->stride_block < c->block_size * c->stride_tok) return SKIPKV_EINVAL;  // the slots of a block must not reach into the next one
+  return SKIPKV_OK;
+}
+
+int quant_rows(const skipkv_quant_cache *qc, const skipkv_cache *rows, int32_t first_layer, const int32_t *begin,
+               const int32_t *end, int32_t *dev_status, void *stream, hipError_t (*launch)(const QuantRowsArgs &, hipStream_t)) {
+  int rc = check_quant(qc);
+  if (rc) return rc;
+  rc = check_cache(rows, false);
+  if (rc) return rc;
+  if (rows->n_kv_heads != qc->n_kv_heads || rows->batch != qc->batch) return SKIPKV_EINVAL;
+  if (first_layer < 0 || (int64_t)first_layer + rows->n_layers > qc->n_layers) return SKIPKV_EINVAL;
+  if (quant_empty(qc) || is_empty(rows) || rows->total_tokens == 0) return SKIPKV_OK;
+  QuantRowsArgs a{};
+  a.k = static_cast<uint8_t *>(qc->k) + first_layer * qc->stride_layer;
+  a.v = static_cast<uint8_t *>(qc->v) + first_layer * qc->stride_layer;
+  a.k_exp = qc->k_exp + (int64_t)first_layer * qc->n_kv_heads * qc->n_blocks;
+  a.v_exp = qc->v_exp + (int64_t)first_layer * qc->n_kv_heads * qc->n_blocks;
+  a.stride_layer = qc->stride_layer;
+  a.stride_head = qc->stride_head;
+  a.stride_block = qc->stride_block;
+  a.stride_tok = qc->stride_tok;
+  a.n_layers = rows->n_layers;
+  a.n_kv_heads = qc->n_kv_heads;
+  a.batch = qc->batch;
+  a.block_log2 = __builtin_ctz((unsigned)qc->block_size);
+  a.n_blocks = qc->n_blocks;
+  a.table_stride = qc->table_stride;
+  a.block_table = qc->block_table;
+  a.rk = rows->k;
+  a.rv = rows->v;
+  a.r_stride_layer = rows->stride_layer;
+  a.r_stride_head = rows->stride_head;
+  a.r_stride_tok = rows->stride_tok;
+  a.dtype = rows->dtype;
+  a.total_tokens = rows->total_tokens;
+  a.seq_off = rows->seq_off;
+  a.begin = begin;
+  a.end = end;
+  a.dev_status = dev_status;
+  return launch(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SKIPKV_OK : SKIPKV_EHIP;
+}
+
+// Checks an attention call and lays it out; *none: it has no output.
+struct AttendLayout {
+  AttendArgs a;
+  size_t o_bytes, total;
+  bool none;
+};
+int resolve_attend(const skipkv_quant_cache *qc, const skipkv_queries *qs, AttendLayout *out) {
+  const int rc = check_quant(qc);
+  if (rc) return rc;
+  if (!qs || (qs->dtype != SKIPKV_F32 && qs->dtype != SKIPKV_BF16)) return SKIPKV_EINVAL;
+  if (qs->total_q < 0 || qs->max_q < 0 || qs->max_len < 0 || qs->n_q_heads < 0) return SKIPKV_EINVAL;
+  if (!(qs->scale - qs->scale == 0.f)) return SKIPKV_EINVAL;  // finite
+  AttendLayout l{};
+  l.none = quant_empty(qc) || qs->total_q == 0 || qs->max_q == 0;
+  if (!l.none) {
+    if (qs->n_q_heads == 0 || qs->n_q_heads % qc->n_kv_heads) return SKIPKV_EINVAL;
+    if (qs->n_q_heads / qc->n_kv_heads > SKIPKV_MAX_GROUP) return SKIPKV_ECAPACITY;
+    if (qs->q_stride_tok < 0 || qs->q_stride_head < 0 || qs->out_stride_tok < 0 || qs->out_stride_head < qc->head_dim) return SKIPKV_EINVAL;
+    if ((qs->q_stride_tok % 8) || (qs->q_stride_head % 8) || (qs->out_stride_tok % 8) || (qs->out_stride_head % 8)) return SKIPKV_EINVAL;
+    AttendArgs &a = l.a;
+    a.stride_head = qc->stride_head;
+    a.stride_block = qc->stride_block;
+    a.stride_tok = qc->stride_tok;
+    a.n_kv_heads = qc->n_kv_heads;
+    a.group = qs->n_q_heads / qc->n_kv_heads;
+    a.batch = qc->batch;
+    a.block_log2 = __builtin_ctz((unsigned)qc->block_size);
+    a.n_blocks = qc->n_blocks;
+    a.table_stride = qc->table_stride;
+    a.block_table = qc->block_table;
+    a.q_off = qs->q_off;
+    a.q = qs->q;
+    a.out = qs->out;
+    a.lse = qs->lse;
+    a.q_stride_tok = qs->q_stride_tok;
+    a.q_stride_head = qs->q_stride_head;
+    a.out_stride_tok = qs->out_stride_tok;
+    a.out_stride_head = qs->out_stride_head;
+    a.dtype = qs->dtype;
+    a.total_q = qs->total_q;
+    a.max_q = std::min(qs->max_q, qs->total_q);
+    // no length above what a table row can hold is accepted
+    a.max_len = (int32_t)std::min<int64_t>(qs->max_len, (int64_t)qc->table_stride * qc->block_size);
+    a.scale = qs->scale;
+    if ((int64_t)a.max_q * a.group > 0x7FFFFF00ll) return SKIPKV_ECAPACITY;  // query rows of a head are 32-bit
+    plan_attend(&a);
+    const int64_t rows = (int64_t)a.total_q * qs->n_q_heads;
+    if ((double)a.batch * a.n_rb * a.n_split * a.n_kv_heads > 2147483647.0 || rows > 4 * 0x7FFFFFFFll) return SKIPKV_ECAPACITY;  // workgroups
+    if (a.n_split > 1) {
+      l.o_bytes = align_up((size_t)a.n_split * (size_t)rows * SKIPKV_HEAD_DIM * sizeof(float));
+      l.total = l.o_bytes + align_up((size_t)a.n_split * (size_t)rows * sizeof(float2));
+    }
+  }
+  *out = l;
+  return SKIPKV_OK;
+}
+}  // namespace
+
+int skipkv_quant_store(const skipkv_quant_cache *qc, const skipkv_cache *rows, int32_t first_layer, const int32_t *begin,
+                       const int32_t *end, int32_t *dev_status, void *stream) {
+  return quant_rows(qc, rows, first_layer, begin, end, dev_status, stream, launch_quant_store);
+}
+
+int skipkv_quant_load(const skipkv_quant_cache *qc, const skipkv_cache *rows, int32_t first_layer, const int32_t *begin,
+                      const int32_t *end, int32_t *dev_status, void *stream) {
+  return quant_rows(qc, rows, first_layer, begin, end, dev_status, stream, launch_quant_load);
+}
+
+int skipkv_quant_attend_workspace_bytes(const skipkv_quant_cache *qc, const skipkv_queries *queries, size_t *out_bytes) {
+  if (!out_bytes) return SKIPKV_EINVAL;
+  AttendLayout l;
+  const int rc = resolve_attend(qc, queries, &l);
+  if (rc) return rc;
+  *out_bytes = l.total;
+  return SKIPKV_OK;
+}
+
+int skipkv_quant_attend(const skipkv_quant_cache *qc, int32_t layer, const skipkv_queries *queries, const int32_t *len,
+                        int32_t *dev_status, void *ws, size_t ws_bytes, void *stream) {
+  AttendLayout l;
+  const int rc = resolve_attend(qc, queries, &l);
+  if (rc) return rc;
+  if (layer < 0 || (layer >= qc->n_layers && qc->n_layers > 0)) return SKIPKV_EINVAL;
+  if (l.none) return SKIPKV_OK;
+  if (!len || !queries->q_off || !queries->q || !queries->out || !aligned16(queries->q) || !aligned16(queries->out) || queries->q == queries->out)
+    return SKIPKV_EINVAL;
+  if (l.total > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < l.total)) return SKIPKV_EWORKSPACE;
+  AttendArgs &a = l.a;
+  a.k = static_cast<const uint8_t *>(qc->k) + layer * qc->stride_layer;
+  a.v = static_cast<const uint8_t *>(qc->v) + layer * qc->stride_layer;
+  a.k_exp = qc->k_exp + (int64_t)layer * qc->n_kv_heads * qc->n_blocks;
+  a.v_exp = qc->v_exp + (int64_t)layer * qc->n_kv_heads * qc->n_blocks;
+  a.len = len;
+  a.dev_status = dev_status;
+  if (l.total > 0) {
+    a.part_o = static_cast<float *>(ws);
+    a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + l.o_bytes);
+  }
+  return launch_attend(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SKIPKV_OK : SKIPKV_EHIP;
+}
+
 int skipkv_steer_add(void *hidden, const void *vec, const float *coef, float coef_scalar, const uint8_t *row_mask,
                      int32_t rows, int32_t d_model, int32_t dtype, void *stream) {
   if (rows < 0 || d_model < 0) return SKIPKV_EINVAL;

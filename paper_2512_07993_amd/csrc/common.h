@@ -336,6 +336,56 @@ struct FuseSharedArgs {
 };
 hipError_t launch_fuse_shared(const FuseSharedArgs &a, hipStream_t st);
 
+// ---- 8-bit cache (quant.hip, attend.hip) and its block tables (pages.hip) -------------------------------
+
+// Rows between a dense cache and the 8-bit pools.  Pool pointers are those of the first layer that is concerned.
+struct QuantRowsArgs {
+  void *k, *v;                   // pools of e4m3 codes
+  uint8_t *k_exp, *v_exp;        // [n_layers, n_kv_heads, n_blocks]
+  int64_t stride_layer, stride_head, stride_block, stride_tok;
+  int32_t n_layers, n_kv_heads, batch, block_log2, n_blocks, table_stride;
+  const int32_t *block_table;
+  const void *rk, *rv;           // dense rows (written by the load)
+  int64_t r_stride_layer, r_stride_head, r_stride_tok;
+  int32_t dtype, total_tokens;
+  const int32_t *seq_off, *begin, *end;  // begin, end: [n_layers, n_kv_heads, batch], nullable
+  int32_t *dev_status;
+};
+hipError_t launch_quant_store(const QuantRowsArgs &a, hipStream_t st);
+hipError_t launch_quant_load(const QuantRowsArgs &a, hipStream_t st);
+
+// Attention of one layer over the 8-bit cache.  Query rows of a (sequence, KV head): row r = j * group + i for query
+// token j and head i of the group, taken in blocks of `rows`; the keys that a block of rows sees are cut into chunks.
+struct AttendArgs {
+  const uint8_t *k, *v, *k_exp, *v_exp;  // of the layer
+  int64_t stride_head, stride_block, stride_tok;
+  int32_t n_kv_heads, group, batch, block_log2, n_blocks, table_stride;
+  const int32_t *block_table, *q_off, *len;  // len: [n_kv_heads, batch]
+  const void *q;
+  void *out;
+  float *lse;
+  int64_t q_stride_tok, q_stride_head, out_stride_tok, out_stride_head;
+  int32_t dtype, total_q, max_q, max_len;
+  float scale;
+  int32_t rows, n_rb;        // query rows per workgroup; blocks of rows per head, at most
+  int32_t chunk, n_split;    // keys per workgroup; chunks per block of rows, at most
+  float *part_o;             // [n_split, total_q, n_q_heads, 128] unnormalised outputs of the chunks
+  float2 *part_ml;           // [n_split, total_q, n_q_heads] (reference, sum), log2 domain
+  int32_t *dev_status;
+};
+void plan_attend(AttendArgs *a);  // fills in rows, n_rb, chunk and n_split
+hipError_t launch_attend(const AttendArgs &a, hipStream_t st);
+
+struct PagesArgs {
+  int32_t *block_table, *n_held, *free_list, *n_free;
+  int32_t batch, table_stride, block_size, n_blocks;
+  const int32_t *len, *new_off;
+  int32_t n_rows, total_new;
+  int32_t *slot_map, *dev_status;
+  int32_t *need, *was_held;  // workspace [batch], [batch + 1]: blocks that a sequence needs (-1: leave it alone); blocks held before, then the free ones
+};
+hipError_t launch_pages_update(const PagesArgs &a, hipStream_t st);
+
 struct SteerArgs {
   void *hidden;
   const void *vec;
