@@ -1305,7 +1305,7 @@ int check_quant(const skipkv_quant_cache *c) {
   if (c->stride_layer < 0 || c->stride_head < 0 || c->stride_tok < c->head_dim) return SKIPKV_EINVAL;
   if ((c->stride_layer % 16) || (c->stride_head % 16) || (c->stride_block % 16) || (c->stride_tok % 16)) return SKIPKV_EINVAL;
   // a block is addressed by 32-bit offsets, positions are 32-bit
-  if (c->stride_tok > (1ll << 31) / 128 - 1 || (int64_t)c->table_stride * c->block_size > 0x7FFFFF00ll) return SKIPKV_ECAPACITY;
+  if (c->stride_tok > (1ll << 31) / 128 - 1 || (int64_t)c->table_stride * c->block_size > (1ll << 30)) return SKIPKV_ECAPACITY;
   if (c->batch > 65535 || (int64_t)c->n_layers * c->n_kv_heads > 32767) return SKIPKV_ECAPACITY;
   if (c->stride_block < c->block_size * c->stride_tok) return SKIPKV_EINVAL;  // the slots of a block must not reach into the next one
   return SKIPKV_OK;
@@ -1396,11 +1396,13 @@ int resolve_attend(const skipkv_quant_cache *qc, const skipkv_queries *qs, Atten
     a.scale = qs->scale;
     if ((int64_t)a.max_q * a.group > 0x7FFFFF00ll) return SKIPKV_ECAPACITY;  // query rows of a head are 32-bit
     plan_attend(&a);
-    const int64_t rows = (int64_t)a.total_q * qs->n_q_heads;
-    if ((double)a.batch * a.n_rb * a.n_split * a.n_kv_heads > 2147483647.0 || rows > 4 * 0x7FFFFFFFll) return SKIPKV_ECAPACITY;  // workgroups
+    // workgroups of a launch (with rows of partial results, one of the join per row at most)
+    const double parts = (double)a.n_entries * a.hw * a.part_rows;
+    if (a.n_rb > 65535 || (double)a.n_split * a.n_kv_heads > 2147483647.0 || (a.n_split > 1 && parts > 2147483647.0)) return SKIPKV_ECAPACITY;
     if (a.n_split > 1) {
-      l.o_bytes = align_up((size_t)a.n_split * (size_t)rows * SKIPKV_HEAD_DIM * sizeof(float));
-      l.total = l.o_bytes + align_up((size_t)a.n_split * (size_t)rows * sizeof(float2));
+      const size_t rows = (size_t)a.n_entries * (size_t)a.n_split * (size_t)a.hw * (size_t)a.part_rows;
+      l.o_bytes = align_up(rows * SKIPKV_HEAD_DIM * sizeof(float));
+      l.total = l.o_bytes + align_up(rows * sizeof(float2));
     }
   }
   *out = l;

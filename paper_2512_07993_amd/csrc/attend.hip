@@ -1,5 +1,6 @@
 // Attention over the 8-bit cache: for every query row r of a (sequence, KV head), out = sum_t p_t v_t with
 // p = softmax(scale * q.k_t) over the keys that the row sees, in one pass over K and V with a running reference and sum.
+// This file: up to 16 rows at a time (decode, drafted tokens), where the cache's bytes are what counts.
 //
 // Everything is computed transposed, so that nothing has to change lanes between the two products: S^T = K Q^T leaves lane (g, c)
 // of a 16 x 16 tile (g = lane / 16, c = lane % 16) with the logits of query row c for keys 4g .. 4g+3, and O^T = V^T P^T wants from that
@@ -14,114 +15,143 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "quant_dev.h"
+#include "attend_dev.h"
 
 namespace skipkv {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kSlack = 8.f;  // the reference may lag behind the maximum by this much (log2): weights up to 2^8, no less accurate
 constexpr int kOPitch = kD + 4;  // floats per row of the merge buffer: 16 rows start at different banks
-
-// How many keys the rows r0 .. r1-1 of a head see: the last of them sees the most.
-__device__ __forceinline__ int rows_see(const AttendArgs &a, int m, int n, int r_last) {
-  return max(0, min(n, n - m + r_last / a.group + 1));
-}
-__device__ __forceinline__ bool seq_queries(const AttendArgs &a, int b, int *q0, int *m) {
-  const int lo = a.q_off[b], hi = a.q_off[b + 1];
-  *q0 = lo;
-  *m = hi - lo;
-  return lo >= 0 && hi >= lo && hi <= a.total_q && hi - lo <= a.max_q;
-}
-__device__ __forceinline__ bool length_ok(const AttendArgs &a, int n) {
-  return n >= 0 && n <= a.max_len && n <= (a.table_stride << a.block_log2);
-}
-
-// x as a sum of N bf16 numbers, the rest of each in the next; pairs of x, y packed.
-template <int N>
-__device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&out)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    out[i] = pack_bf16x2(x, y);
-    if (i + 1 < N) {
-      x -= __uint_as_float(out[i] << 16);
-      y -= __uint_as_float(out[i] & 0xFFFF0000u);
-    }
-  }
-}
-__device__ __forceinline__ bf16x8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d)); }
-
-__device__ __forceinline__ float nan32() { return __uint_as_float(0x7FC00000u); }
-// Bytes of w that are a NaN code (0x7F, 0xFF), as 0xFF.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-  const uint32_t high = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // 0x7F + 1: no carry leaves a byte
-  return (high >> 7) * 0xFFu;
-}
-__device__ __forceinline__ bool has_nan(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0; }
-
-// Four dimensions of a finished row (d = 0: and its lse): v / all, rounded once.
-template <int DT>
-__device__ __forceinline__ void store_row(const AttendArgs &a, int tok, int head, int64_t row, int d, float4 v, float top, float all) {
-  const bool none = all == 0.f;  // the row sees no key
-  const float f = none ? 0.f : 1.f / all;
-  const float4 y = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-  const int64_t at = tok * a.out_stride_tok + head * a.out_stride_head + d;
-  if constexpr (DT == SKIPKV_BF16) *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
-  else *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = y;
-  if (d == 0 && a.lse) a.lse[row] = none ? -__builtin_inff() : (top + log2f(all)) * kLn2;
-}
-
+constexpr int kWaves = 8;        // per workgroup; two workgroups share a CU (one with fp32 queries)
 // 32 keys of a wave: two tiles of 16, each within one block.
 struct Keys {
   uint4 k[2][2];  // [tile][piece]
+};
+struct Values {
   uint2 v[2][4];  // [tile][key 4g + i]
 };
 
-// DT: type of q and out.  QT: tiles of 16 query rows.  W: waves, which take the steps of 32 keys in turn.
+// The 8 operands (tiles of dimensions { 8m + j }) that a wave's values make.
+template <class Code, class Use>
+__device__ __forceinline__ void value_frags(const Values &kv, const float (&scale)[2], Code &&code, Use &&use) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {  // dimensions 8c + 4 half + (0 .. 3)
+    uint32_t w[4][2];  // [pair of keys][two dimensions]: codes of both keys side by side
+#pragma unroll
+    for (int pr = 0; pr < 4; ++pr) {
+      const uint2 u0 = kv.v[pr >> 1][2 * (pr & 1)], u1 = kv.v[pr >> 1][2 * (pr & 1) + 1];
+      const uint32_t a0 = code(half ? u0.y : u0.x), a1 = code(half ? u1.y : u1.x);
+      w[pr][0] = __builtin_amdgcn_perm(a1, a0, 0x05010400u);
+      w[pr][1] = __builtin_amdgcn_perm(a1, a0, 0x07030602u);
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      uint32_t f[4];
+#pragma unroll
+      for (int pr = 0; pr < 4; ++pr)
+        f[pr] = d & 1 ? e4m3_to_bf16x2<true>(w[pr][d >> 1], scale[pr >> 1]) : e4m3_to_bf16x2<false>(w[pr][d >> 1], scale[pr >> 1]);
+      use(4 * half + d, frag(f[0], f[1], f[2], f[3]));
+      if (d & 1) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+
+// HW: heads side by side (their rows of a slot are neighbours in memory: 512 bytes at a time come faster than 128), one or more waves to
+// each, which take steps of 32 keys in turn.  DT: type of q and out.
 // Accuracy: stored keys and values are bf16 numbers.  bf16 queries enter as they are; fp32 ones as three bf16 parts (24 bits).  Weights
 // enter the second product as two parts (16 bits) with bf16 outputs, three with fp32 ones.  Everything else is fp32.
-template <int DT, int QT, int W>
-__global__ void __launch_bounds__(64 * W) k_attend(AttendArgs a) {
+template <int DT, int HW>
+__global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_attend(AttendArgs a) {
+  constexpr int KW = kWaves / HW;
   constexpr int NQ = DT == SKIPKV_BF16 ? 1 : 3, NP = DT == SKIPKV_BF16 ? 2 : 3;
   constexpr int ESZ = DT == SKIPKV_BF16 ? 2 : 4;
-  __shared__ __align__(16) float o_part[W][16][kOPitch];
-  __shared__ float2 ml_part[W][16];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-  // ---- which rows and keys
-  uint32_t x = blockIdx.x;
-  const int h = x % a.n_kv_heads;
-  x /= a.n_kv_heads;
-  const int split = x % a.n_split;
-  x /= a.n_split;
-  const int rb = x % a.n_rb, b = x / a.n_rb;
+  __shared__ __align__(16) float o_part[kWaves][16][kOPitch];
+  __shared__ float2 ml_part[kWaves][16];
+  const int tid = threadIdx.x, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave_all / HW, hw = wave_all % HW;
+  const int lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int bmask = (1 << a.block_log2) - 1;
+  const int n_hg = a.n_kv_heads / HW, split = blockIdx.x / n_hg, hg = blockIdx.x - split * n_hg, h = hg * HW + hw;
+  const int rb = blockIdx.y, b = blockIdx.z;
+  const int k_begin = split * a.chunk;
+  const int32_t *table = a.block_table + (int64_t)b * a.table_stride;
+  // Up to 32 steps at a time: lane i looks up the block of tile i & 1 of step i >> 1.  The first look-up waits for nothing: what it
+  // finds behind the last key is put right below.
+  auto tile_key = [&](int s0) { return k_begin + ((s0 + (lane >> 1)) * KW + kw) * 32 + (lane & 1) * 16; };
+  int id = 0;
+  {
+    const int at = tile_key(0) >> a.block_log2;
+    if (at < a.table_stride) id = table[at];
+  }
+  int n = 0, most = 0;  // keys of this head; keys that some head of the group sees
+  bool n_ok = true;
   int q0, m;
-  if (!seq_queries(a, b, &q0, &m)) {
-    if (split == 0 && rb == 0 && tid == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
+  const bool q_ok = seq_queries(a, b, &q0, &m);
+  const int r0 = rb * a.rows, r1 = min(r0 + a.rows, m * a.group);
+#pragma unroll
+  for (int i = 0; i < HW; ++i) {
+    const int ni = a.len[(hg * HW + i) * a.batch + b];
+    const bool ok = length_ok(a, ni);
+    most = max(most, ok ? rows_see(a, m, ni, r1 - 1) : 0);
+    if (i == hw) {
+      n = ni;
+      n_ok = ok;
+    }
+  }
+  const int n_chunks = max(1, (most + a.chunk - 1) / a.chunk);
+  if (!q_ok || r0 >= r1 || split >= n_chunks) {
+    if (!q_ok && split == 0 && rb == 0 && lane == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
     return;
   }
-  const int r0 = rb * a.rows, r1 = min(r0 + a.rows, m * a.group);
-  if (r0 >= r1) return;
-  const int n = a.len[h * a.batch + b];
-  const bool n_ok = length_ok(a, n);
-  if (!n_ok) {
-    if (split > 0) return;
-    if (tid == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
-  }
-  const int k_end_all = n_ok ? rows_see(a, m, n, r1 - 1) : 0;
-  const int n_chunks = max(1, (k_end_all + a.chunk - 1) / a.chunk);
-  if (split >= n_chunks) return;
-  const int k_begin = split * a.chunk, k_end = min(k_end_all, k_begin + a.chunk);
-
-  // ---- queries: lane (g, c) holds dimensions 64 i + 16 g + 8 half + (0 .. 7) of row c of every tile
-  bf16x8 qf[QT][NQ][4];
-  int sees[QT];  // keys that row c of the tile sees
+  if (!n_ok && split == 0 && lane == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
+  const int k_end = min(n_ok ? rows_see(a, m, n, r1 - 1) : 0, k_begin + a.chunk);
+  const int steps_all = max(0, (k_end - k_begin + 31) / 32);
+  const int steps = kw < steps_all ? (steps_all - kw + KW - 1) / KW : 0;  // of this wave
+  bool poison = !n_ok;
+  auto check_id = [&](int s0) {
+    const bool in = tile_key(s0) < k_end, good = id >= 0 && id < a.n_blocks;
+    poison |= in && !good;
+    if (!in || !good) id = 0;
+  };
+  check_id(0);
+  const uint8_t *kbase = a.k + h * a.stride_head, *vbase = a.v + h * a.stride_head;
+  const uint8_t *kexp = a.k_exp + (int64_t)h * a.n_blocks, *vexp = a.v_exp + (int64_t)h * a.n_blocks;
+  const uint32_t k_lane = (uint32_t)c * (uint32_t)a.stride_tok + 16 * g;
+  const uint32_t v_lane = (uint32_t)(4 * g) * (uint32_t)a.stride_tok + 8 * c;
+  auto row_of = [&](int s0, int s, int t) {  // (tiles that lie behind the last key read block 0)
+    const int key = k_begin + ((s0 + s) * KW + kw) * 32 + t * 16;
+    return (int64_t)__builtin_amdgcn_readlane(id, 2 * s + t) * a.stride_block + (int64_t)(key & bmask) * a.stride_tok;
+  };
+  Keys kk;
+  Values kv;
+  auto load_k = [&](int s0, int s) {
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = r0 + 16 * t + c;
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t *p = kbase + row_of(s0, s, t);
+      kk.k[t][0] = *reinterpret_cast<const uint4 *>(p + k_lane);
+      kk.k[t][1] = *reinterpret_cast<const uint4 *>(p + k_lane + 64);
+    }
+  };
+  auto load_v = [&](int s0, int s) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t *p = vbase + row_of(s0, s, t);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kv.v[t][i] = *reinterpret_cast<const uint2 *>(p + v_lane + (uint32_t)i * (uint32_t)a.stride_tok);
+    }
+  };
+  load_k(0, 0);
+  load_v(0, 0);
+  uint32_t ke = kexp[id], ve = vexp[id];
+
+  // ---- queries: lane (g, c) holds dimensions 64 i + 16 g + 8 half + (0 .. 7) of row c
+  bf16x8 qf[NQ][4];
+  int sees = 0x7FFFFFFF;  // keys that row c sees
+  {
+    const uint32_t q_sign = a.scale < 0.f ? 0x80008000u : 0u;
+    const int r = r0 + c, j = r / a.group, i = r - j * a.group;
     const bool in = r < r1;
-    const int j = r / a.group, i = r - j * a.group;
-    sees[t] = in ? n - m + j + 1 : 0x7FFFFFFF;
+    if (in) sees = n - m + j + 1;
     const char *p = static_cast<const char *>(a.q) + ((q0 + j) * a.q_stride_tok + (h * a.group + i) * a.q_stride_head + 16 * g) * ESZ;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -129,315 +159,328 @@ __global__ void __launch_bounds__(64 * W) k_attend(AttendArgs a) {
       if (in) {
         const char *src = p + (64 * (s >> 1) + 8 * (s & 1)) * ESZ;
         if constexpr (DT == SKIPKV_BF16) {
-          const uint4 u = *reinterpret_cast<const uint4 *>(src);
-          w[0][0] = u.x, w[0][1] = u.y, w[0][2] = u.z, w[0][3] = u.w;
+          const uint4 x = *reinterpret_cast<const uint4 *>(src);
+          w[0][0] = x.x, w[0][1] = x.y, w[0][2] = x.z, w[0][3] = x.w;
         } else {
-          const float4 u = reinterpret_cast<const float4 *>(src)[0], v = reinterpret_cast<const float4 *>(src)[1];
-          const float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+          const float4 x = reinterpret_cast<const float4 *>(src)[0], y = reinterpret_cast<const float4 *>(src)[1];
+          const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int i4 = 0; i4 < 4; ++i4) {
             uint32_t parts[NQ];
-            split_bf16(f[2 * e], f[2 * e + 1], parts);
+            split_bf16(f[2 * i4], f[2 * i4 + 1], parts);
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) w[k][e] = parts[k];
+            for (int k = 0; k < NQ; ++k) w[k][i4] = parts[k];
           }
         }
       }
 #pragma unroll
-      for (int k = 0; k < NQ; ++k) qf[t][k][s] = frag(w[k][0], w[k][1], w[k][2], w[k][3]);
+      for (int k = 0; k < NQ; ++k) qf[k][s] = frag(w[k][0] ^ q_sign, w[k][1] ^ q_sign, w[k][2] ^ q_sign, w[k][3] ^ q_sign);
     }
   }
   const int all_see = max(0, n - m + r0 / a.group + 1);  // keys below this are seen by every row
 
-  f32x4 o[QT][8];
-  float ref[QT], sum[QT];
+  f32x4 o[8];
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    ref[t] = kRefInit;
-    sum[t] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  const float to_log2 = a.scale * kLog2e;
-  bool poison = !n_ok;
-
-  const uint8_t *kbase = a.k + h * a.stride_head, *vbase = a.v + h * a.stride_head;
-  const uint8_t *kexp = a.k_exp + (int64_t)h * a.n_blocks, *vexp = a.v_exp + (int64_t)h * a.n_blocks;
-  const int32_t *table = a.block_table + (int64_t)b * a.table_stride;
-  const int bmask = (1 << a.block_log2) - 1;
-  const uint32_t k_lane = (uint32_t)c * (uint32_t)a.stride_tok + 16 * g;
-  const uint32_t v_lane = (uint32_t)(4 * g) * (uint32_t)a.stride_tok + 8 * c;
-  const int steps_all = (k_end - k_begin + 31) / 32;
-  const int steps = wave < steps_all ? (steps_all - wave + W - 1) / W : 0;  // of this wave
-
-  // Up to 32 steps at a time: lane i looks up the block of tile i & 1 of step i >> 1, and its scales.
+  for (int j = 0; j < 8; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float ref = kRefInit, sum = 0.f;
+  // (the scale's sign has gone into the queries; not 0, so that what is not seen stays -inf)
+  const float to_log2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-45f);
+  int nan_from = 0x7FFFFFFF;  // first step of the wave with a NaN that only some rows see
   for (int s0 = 0; s0 < steps; s0 += 32) {
-    int id = 0;
-    float ks = 1.f, vs = 1.f;
-    {
-      const int key = k_begin + ((s0 + (lane >> 1)) * W + wave) * 32 + (lane & 1) * 16;
-      if (key < k_end) {
-        id = table[key >> a.block_log2];
-        if (id < 0 || id >= a.n_blocks) {
-          poison = true;
-          id = 0;
-        }
-        ks = scale_of_byte(kexp[id]);
-        vs = scale_of_byte(vexp[id]);
-      }
+    if (s0 > 0) {
+      const int key = tile_key(s0);
+      id = key < k_end ? table[key >> a.block_log2] : 0;
+      check_id(s0);
+      load_k(s0, 0);
+      load_v(s0, 0);
+      ke = kexp[id];
+      ve = vexp[id];
     }
-    auto load = [&](int s) {  // (tiles that lie behind the last key read block 0)
-      Keys kv;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int key = k_begin + ((s0 + s) * W + wave) * 32 + t * 16;
-        const int64_t row = (int64_t)__builtin_amdgcn_readlane(id, 2 * s + t) * a.stride_block + (int64_t)(key & bmask) * a.stride_tok;
-        const uint8_t *kp = kbase + row, *vp = vbase + row;
-        kv.k[t][0] = *reinterpret_cast<const uint4 *>(kp + k_lane);
-        kv.k[t][1] = *reinterpret_cast<const uint4 *>(kp + k_lane + 64);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kv.v[t][i] = *reinterpret_cast<const uint2 *>(vp + v_lane + (uint32_t)i * (uint32_t)a.stride_tok);
-      }
-      return kv;
-    };
     const int here = min(32, steps - s0);
-    Keys next = load(0);
     for (int s = 0; s < here; ++s) {
-      Keys kv = next;
-      if (s + 1 < here) next = load(s + 1);
-      const int key0 = k_begin + ((s0 + s) * W + wave) * 32;
-      const float ks2[2] = {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), 2 * s)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), 2 * s + 1))};
-      const float vs2[2] = {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), 2 * s)), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), 2 * s + 1))};
-      const bool whole = key0 + 32 <= min(all_see, k_end);  // every row sees every key
+      const int after = min(s + 1, here - 1);  // loaded as soon as the registers are free (the last one again)
+      const int key0 = k_begin + ((s0 + s) * KW + kw) * 32;
+      const float ks2[2] = {scale_of_byte(__builtin_amdgcn_readlane(ke, 2 * s)), scale_of_byte(__builtin_amdgcn_readlane(ke, 2 * s + 1))};
+      const float vs2[2] = {scale_of_byte(__builtin_amdgcn_readlane(ve, 2 * s)), scale_of_byte(__builtin_amdgcn_readlane(ve, 2 * s + 1))};
+      const bool all_seen = key0 + 32 <= min(all_see, k_end);
       // ---- logits
-      f32x4 acc[QT][2];
+      f32x4 acc[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         bf16x8 kf[4];
 #pragma unroll
         for (int s4 = 0; s4 < 4; ++s4) {
-          const uint4 u = kv.k[t][s4 >> 1];
-          const uint32_t w0 = s4 & 1 ? u.z : u.x, w1 = s4 & 1 ? u.w : u.y;
+          const uint4 x = kk.k[t][s4 >> 1];
+          const uint32_t w0 = s4 & 1 ? x.z : x.x, w1 = s4 & 1 ? x.w : x.y;
           kf[s4] = frag(e4m3_to_bf16x2<false>(w0, ks2[t]), e4m3_to_bf16x2<true>(w0, ks2[t]), e4m3_to_bf16x2<false>(w1, ks2[t]), e4m3_to_bf16x2<true>(w1, ks2[t]));
         }
+        f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < QT; ++q) {
-          f32x4 z = {0.f, 0.f, 0.f, 0.f};
+        for (int k = NQ - 1; k >= 0; --k)
 #pragma unroll
-          for (int k = NQ - 1; k >= 0; --k)
-#pragma unroll
-            for (int s4 = 0; s4 < 4; ++s4) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s4], qf[q][k][s4], z, 0, 0, 0);
-          acc[q][t] = z * to_log2;
-        }
+          for (int s4 = 0; s4 < 4; ++s4) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s4], qf[k][s4], z, 0, 0, 0);
+        acc[t] = z;
+        __builtin_amdgcn_sched_barrier(0);  // (few registers: four waves share a SIMD)
       }
+      load_k(s0, after);
       // ---- what is not seen
-      bool v_nan = false;
-      if (!whole) {
+      if (!all_seen) {
+        asm volatile("");  // (a branch: this is not worth computing for every step)
+        bool v_nan = false;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int key = key0 + 16 * t + 4 * g + i;
-            if (key >= k_end) kv.v[t][i] = make_uint2(0, 0);
-            v_nan |= has_nan(kv.v[t][i].x) || has_nan(kv.v[t][i].y);
-#pragma unroll
-            for (int q = 0; q < QT; ++q)
-              if (key >= min(sees[q], k_end)) acc[q][t][i] = -__builtin_inff();
+            uint2 &x = kv.v[t][i];
+            if (key >= k_end) x = make_uint2(0, 0);
+            v_nan |= has_nan(x.x) || has_nan(x.y);
+            x = make_uint2(x.x & ~nan_bytes(x.x), x.y & ~nan_bytes(x.y));  // (see below)
+            if (key >= min(sees, k_end)) acc[t][i] = -__builtin_inff();
           }
-        v_nan = __any(v_nan);
+        if (__any(v_nan)) nan_from = min(nan_from, s0 + s);
       }
       // ---- weights
-      uint32_t pf[QT][NP][4];
+      uint32_t pf[NP][4];
+      {
+        float top = acc[0][0];
 #pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        float top = acc[q][0][0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, acc[q][i >> 2][i & 3]);
-        if (__any(top > ref[q] + kSlack)) {
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, acc[i >> 2][i & 3]);
+        top *= to_log2;
+        if (__any(top > ref + kSlack)) {
+          asm volatile("");
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float now = fmaxf(ref[q], top), f = __builtin_amdgcn_exp2f(ref[q] - now);
-          ref[q] = now;
-          sum[q] *= f;
+          const float now = fmaxf(ref, top), f = __builtin_amdgcn_exp2f(ref - now);
+          ref = now;
+          sum *= f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[q][j] *= f;
+          for (int j = 0; j < 8; ++j) o[j] *= f;
         }
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(acc[q][i >> 2][i & 3] - ref[q]);
-          sum[q] += p[i];
+          p[i] = __builtin_amdgcn_exp2f(fmaf(acc[i >> 2][i & 3], to_log2, -ref));
+          sum += p[i];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t parts[NP];
           split_bf16(p[2 * i], p[2 * i + 1], parts);
 #pragma unroll
-          for (int k = 0; k < NP; ++k) pf[q][k][i] = parts[k];
+          for (int k = 0; k < NP; ++k) pf[k][i] = parts[k];
         }
       }
-      // ---- values, and where a NaN among them is seen
-      auto product = [&](auto &&use) {
+      // ---- values
+      value_frags(kv, vs2, [](uint32_t w) { return w; }, [&](int j, bf16x8 vf) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {  // dimensions 8c + 4 half + (0 .. 3)
-          uint32_t w[4][2];  // [pair of keys][two dimensions]: codes of both keys side by side
-#pragma unroll
-          for (int pr = 0; pr < 4; ++pr) {
-            const uint2 u0 = kv.v[pr >> 1][2 * (pr & 1)], u1 = kv.v[pr >> 1][2 * (pr & 1) + 1];
-            const uint32_t a0 = half ? u0.y : u0.x, a1 = half ? u1.y : u1.x;
-            w[pr][0] = __builtin_amdgcn_perm(a1, a0, 0x05010400u);
-            w[pr][1] = __builtin_amdgcn_perm(a1, a0, 0x07030602u);
-          }
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            uint32_t f[4];
-#pragma unroll
-            for (int pr = 0; pr < 4; ++pr) f[pr] = d & 1 ? e4m3_to_bf16x2<true>(w[pr][d >> 1], vs2[pr >> 1]) : e4m3_to_bf16x2<false>(w[pr][d >> 1], vs2[pr >> 1]);
-            use(4 * half + d, frag(f[0], f[1], f[2], f[3]));
-          }
-        }
-      };
-      if (v_nan) {
-        // A weight of 0 does not undo a NaN in a matrix product, so here NaN are taken out of the values and counted apart, with
-        // weight 1 for the rows that see them.
-        Keys clean = kv;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            clean.v[t][i] = make_uint2(kv.v[t][i].x & ~nan_bytes(kv.v[t][i].x), kv.v[t][i].y & ~nan_bytes(kv.v[t][i].y));
-            kv.v[t][i] = make_uint2(nan_bytes(kv.v[t][i].x) & 0x38383838u, nan_bytes(kv.v[t][i].y) & 0x38383838u);  // 0x38: 1.0
-          }
-        product([&](int j, bf16x8 vf) {
-#pragma unroll
-          for (int q = 0; q < QT; ++q) {
-            uint32_t one[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = key0 + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
-              one[i] = (key < min(sees[q], k_end) ? 0x3F80u : 0u) | (key + 1 < min(sees[q], k_end) ? 0x3F800000u : 0u);
-            }
-            const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(one[0], one[1], one[2], one[3]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (z[i] > 0.f) o[q][j][i] = nan32();
-          }
-        });
-        kv = clean;
-      }
-      product([&](int j, bf16x8 vf) {
-#pragma unroll
-        for (int q = 0; q < QT; ++q)
-#pragma unroll
-          for (int k = NP - 1; k >= 0; --k)
-            o[q][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(pf[q][k][0], pf[q][k][1], pf[q][k][2], pf[q][k][3]), o[q][j], 0, 0, 0);
+        for (int k = NP - 1; k >= 0; --k) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(pf[k][0], pf[k][1], pf[k][2], pf[k][3]), o[j], 0, 0, 0);
       });
+      load_v(s0, after);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  }
+  // A weight of 0 does not undo a NaN in a matrix product, so NaN have been taken out of the values of the steps that not every row sees
+  // in full; here they are counted, with weight 1 for the rows that see them.
+  for (int s = nan_from; s < steps; ++s) {
+    const int key0 = k_begin + (s * KW + kw) * 32;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + 16 * t + 4 * g + i;
+        const int p = key < k_end ? table[key >> a.block_log2] : -1;
+        kv.v[t][i] = make_uint2(0, 0);
+        if (p >= 0 && p < a.n_blocks) kv.v[t][i] = *reinterpret_cast<const uint2 *>(vbase + p * a.stride_block + (int64_t)(key & bmask) * a.stride_tok + 8 * c);
+      }
+    uint32_t one[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = key0 + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+      one[i] = (key < min(sees, k_end) ? 0x3F80u : 0u) | (key + 1 < min(sees, k_end) ? 0x3F800000u : 0u);
+    }
+    const float unscaled[2] = {1.f, 1.f};
+    value_frags(kv, unscaled, [](uint32_t w) { return nan_bytes(w) & 0x38383838u; /* the code of 1 */ }, [&](int j, bf16x8 vf) {
+      const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(one[0], one[1], one[2], one[3]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (z[i] > 0.f) o[j][i] = nan32();
+    });
   }
   poison = __any(poison);
   if (poison && n_ok && lane == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_BLOCK_TABLE);
 
-  // ---- merge of the waves, a tile of rows at a time
+  // ---- merge of a head's waves: lane (g, c) has row c, dimensions 32 g + 8 i + j
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (g == 0) ml_part[wave_all][c] = make_float2(ref, poison ? nan32() : sum);
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    if (t) __syncthreads();
-    float l = sum[t];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (g == 0) ml_part[wave][c] = make_float2(ref[t], poison ? nan32() : l);
-    // lane (g, c): row c, dimensions 32 g + 8 i + j
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int j4 = 0; j4 < 2; ++j4)
+      *reinterpret_cast<float4 *>(&o_part[wave_all][c][32 * g + 8 * i + 4 * j4]) = make_float4(o[4 * j4][i], o[4 * j4 + 1][i], o[4 * j4 + 2][i], o[4 * j4 + 3][i]);
+  __syncthreads();
+  const int rows = r1 - r0, entry = (b * a.n_rb + rb) * n_hg + hg;
+  for (int item = kw * 64 + lane; item < rows * (kD / 4); item += 64 * KW) {
+    const int row = item / (kD / 4), d = 4 * (item % (kD / 4)), r = r0 + row;
+    float top = kRefInit;
 #pragma unroll
-      for (int j4 = 0; j4 < 2; ++j4)
-        *reinterpret_cast<float4 *>(&o_part[wave][c][32 * g + 8 * i + 4 * j4]) = make_float4(o[t][4 * j4][i], o[t][4 * j4 + 1][i], o[t][4 * j4 + 2][i], o[t][4 * j4 + 3][i]);
-    __syncthreads();
-    for (int item = tid; item < 16 * (kD / 4); item += 64 * W) {
-      const int row = item / (kD / 4), d = 4 * (item % (kD / 4)), r = r0 + 16 * t + row;
-      if (r >= r1) break;
-      float top = kRefInit;
+    for (int w = 0; w < KW; ++w) top = fmaxf(top, ml_part[w * HW + hw][row].x);
+    float all = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < W; ++w) top = fmaxf(top, ml_part[w][row].x);
-      float all = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = 0; w < KW; ++w) {
+      const float2 ml = ml_part[w * HW + hw][row];
+      const float f = __builtin_amdgcn_exp2f(ml.x - top);
+      const float4 x = *reinterpret_cast<const float4 *>(&o_part[w * HW + hw][row][d]);
+      all += ml.y * f;
+      v.x += x.x * f, v.y += x.y * f, v.z += x.z * f, v.w += x.w * f;
+    }
+    if (n_chunks == 1) {
+      const int j = r / a.group;
+      store_row<DT>(a, q0 + j, h * a.group + r - j * a.group, d, v, top, all);
+    } else {
+      const int64_t at = (((int64_t)entry * a.n_split + split) * HW + hw) * a.part_rows + row;
+      *reinterpret_cast<float4 *>(a.part_o + at * kD + d) = v;
+      if (d == 0) a.part_ml[at] = make_float2(top, all);
+    }
+  }
+}
+
+// Entries (sequence, block of rows, group of heads) of several chunks: 32 lanes per chunk of a row, four dimensions each, GR chunks at a
+// time; a workgroup has 8 / GR rows.  What it costs is waiting for memory, so all chunks up to 8 * GR are under way together,
+// before it is known how many there are.
+template <int DT, int GR>
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
+  __shared__ float4 v_part[8][32];
+  __shared__ float2 ml_part[8];
+  const int tid = threadIdx.x, d = tid & 31, grp = (tid >> 5) % GR, n_hg = a.n_kv_heads / a.hw;
+  const int64_t row_at = (int64_t)blockIdx.x * (8 / GR) + (tid >> 5) / GR;  // (entry, head of the group, row)
+  const int per_entry = a.hw * a.part_rows;
+  const int64_t entry = row_at / per_entry;
+  const int in_entry = (int)(row_at - entry * per_entry);
+  const bool in = entry < a.n_entries;
+  constexpr int AHEAD = 8;
+  float2 ml[AHEAD];
+  float4 x[AHEAD];
+  auto fetch = [&](int s0) {
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float2 ml = ml_part[w][row];
-        const float f = __builtin_amdgcn_exp2f(ml.x - top);
-        const float4 u = *reinterpret_cast<const float4 *>(&o_part[w][row][d]);
-        all += ml.y * f;
-        v.x += u.x * f, v.y += u.y * f, v.z += u.z * f, v.w += u.w * f;
+    for (int i = 0; i < AHEAD; ++i) {
+      const int s = s0 + i * GR + grp;
+      if (in && s < a.n_split) {
+        const int64_t at = (entry * a.n_split + s) * per_entry + in_entry;
+        ml[i] = a.part_ml[at];
+        x[i] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + 4 * d);
       }
-      const int j = r / a.group, head = h * a.group + r - j * a.group;
-      const int64_t row_all = (int64_t)(q0 + j) * a.n_kv_heads * a.group + head;
-      if (n_chunks > 1) {
-        const int64_t at = (int64_t)split * a.total_q * a.n_kv_heads * a.group + row_all;
-        *reinterpret_cast<float4 *>(a.part_o + at * kD + d) = v;
-        if (d == 0) a.part_ml[at] = make_float2(top, all);
-      } else {
-        store_row<DT>(a, q0 + j, head, row_all, d, v, top, all);
+    }
+  };
+  fetch(0);
+  const int hw = in_entry / a.part_rows, hg = (int)(entry % n_hg), b = (int)(entry / n_hg / a.n_rb), rb = (int)(entry / n_hg % a.n_rb);
+  const int r = rb * a.rows + in_entry - hw * a.part_rows;
+  int n_chunks = 0, q0 = 0;
+  if (in) {
+    int m;
+    const bool q_ok = seq_queries(a, b, &q0, &m);
+    const int r1 = min((rb + 1) * a.rows, m * a.group);
+    int most = 0;
+    for (int i = 0; i < a.hw; ++i) {
+      const int n = a.len[(hg * a.hw + i) * a.batch + b];
+      if (length_ok(a, n)) most = max(most, rows_see(a, m, n, r1 - 1));
+    }
+    if (q_ok && r < r1) n_chunks = (most + a.chunk - 1) / a.chunk;
+  }
+  if (n_chunks <= 1) n_chunks = 0;  // written already
+  if (GR == 8 && n_chunks == 0) return;
+  float top = kRefInit, all = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 < n_chunks;) {
+    float now = top;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (s0 + i * GR + grp < n_chunks) now = fmaxf(now, ml[i].x);
+    const float back = __builtin_amdgcn_exp2f(top - now);
+    top = now;
+    all *= back;
+    v.x *= back, v.y *= back, v.z *= back, v.w *= back;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (s0 + i * GR + grp < n_chunks) {
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - now);
+        all += ml[i].y * f;
+        v.x += x[i].x * f, v.y += x[i].y * f, v.z += x[i].z * f, v.w += x[i].w * f;
+      }
+    s0 += AHEAD * GR;
+    if (s0 < n_chunks) fetch(s0);
+  }
+  if constexpr (GR > 1) {
+    v_part[tid >> 5][d] = v;
+    if (d == 0) ml_part[tid >> 5] = make_float2(top, all);
+    __syncthreads();
+    if (grp > 0) return;
+    const int g0 = tid >> 5;
+#pragma unroll
+    for (int i = 1; i < GR; ++i) top = fmaxf(top, ml_part[g0 + i].x);
+    all = 0.f;
+    v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < GR; ++i) {
+      const float f = __builtin_amdgcn_exp2f(ml_part[g0 + i].x - top);
+      const float4 w = v_part[g0 + i][d];
+      all += ml_part[g0 + i].y * f;
+      v.x += w.x * f, v.y += w.y * f, v.z += w.z * f, v.w += w.w * f;
+    }
+  }
+  if (n_chunks == 0) return;
+  const int j = r / a.group;
+  store_row<DT>(a, q0 + j, (hg * a.hw + hw) * a.group + r - j * a.group, 4 * d, v, top, all);
+}
+
+}  // namespace
+
+// How the work is laid out: heads side by side, and chunks per entry.  A workgroup's unit is one step of its 8 waves, 64 KB of codes
+// whatever their number of heads; a CU takes some 2.9 us for it when the whole chip reads (3.05 and 3.3 us where two heads' rows or one's
+// lie together), the way to the first unit and from the last costs 4 us, joining chunks a launch of 5 us.  Taken is what comes out
+// shortest if all lengths were max_len.  Measured, us, one head / four heads side by side, chunks as the rule has them:
+//   64 x 4 heads, 1152 keys 15.8 / 22.5;  50 x 8 heads, 400-830 keys 18.6 / 22.8;  1 x 8 heads, 4224 keys 11.2 / 12.3;
+//   8 x 8 heads, 32896 keys 127 / 104;  18 x 8 heads, 10 K keys 110 / 74.
+void plan_attend(AttendArgs *a) {
+  a->rows = 16;
+  a->n_rb = (int32_t)(((int64_t)a->max_q * a->group + a->rows - 1) / a->rows);
+  a->part_rows = (int32_t)std::min<int64_t>(a->rows, (int64_t)a->max_q * a->group);
+  double best = 0;
+  for (const int hw : {4, 2, 1}) {
+    if (a->n_kv_heads % hw) continue;
+    const int unit = 32 * kWaves / hw, units = std::max(1, (a->max_len + unit - 1) / unit);
+    const int64_t entries = (int64_t)a->batch * a->n_rb * (a->n_kv_heads / hw);
+    for (int per = units; per >= 1; per = std::min(per - 1, per * 7 / 8)) {  // units per workgroup
+      const int split = (units + per - 1) / per;
+      const double turns = (double)((entries * split + 255) / 256);
+      const double us = turns * (per * (hw == 4 ? 2.9 : hw == 2 ? 3.05 : 3.3) + 4) + (split > 1 ? 5 : 0);
+      if (best == 0 || us < best) {
+        best = us;
+        a->hw = hw;
+        a->chunk = per * unit;
+        a->n_split = split;
+        a->n_entries = entries;
       }
     }
   }
 }
 
-// Rows whose keys were cut into chunks: a wave per row, two dimensions per lane.
-template <int DT>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
-  const int n_heads = a.n_kv_heads * a.group, lane = threadIdx.x & 63;
-  const int64_t rows = (int64_t)a.total_q * n_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int tok = (int)(row / n_heads), head = (int)(row - (int64_t)tok * n_heads);
-  int lo = 0, hi = a.batch;  // the last sequence that begins at or before the token
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.q_off[mid] <= tok) lo = mid;
-    else hi = mid;
-  }
-  int q0, m;
-  if (!seq_queries(a, lo, &q0, &m) || tok < q0 || tok >= q0 + m) return;
-  const int h = head / a.group, n = a.len[h * a.batch + lo];
-  if (!length_ok(a, n)) return;
-  const int r = (tok - q0) * a.group + head % a.group, r1 = min((r / a.rows + 1) * a.rows, m * a.group);
-  const int n_chunks = (rows_see(a, m, n, r1 - 1) + a.chunk - 1) / a.chunk;
-  if (n_chunks <= 1) return;
-  float top = kRefInit, all = 0.f;
-  for (int s = 0; s < n_chunks; ++s) top = fmaxf(top, a.part_ml[s * rows + row].x);
-  float2 v = make_float2(0.f, 0.f);
-  for (int s = 0; s < n_chunks; ++s) {
-    const float2 ml = a.part_ml[s * rows + row];
-    const float f = __builtin_amdgcn_exp2f(ml.x - top);
-    const float2 u = *reinterpret_cast<const float2 *>(a.part_o + (s * rows + row) * kD + 2 * lane);
-    all += ml.y * f;
-    v.x += u.x * f, v.y += u.y * f;
-  }
-  const float4 w = make_float4(v.x, v.y, __shfl_down(v.x, 1), __shfl_down(v.y, 1));
-  if (!(lane & 1)) store_row<DT>(a, tok, head, row, 2 * lane, w, top, all);
-}
-
-}  // namespace
-
-void plan_attend(AttendArgs *a) {
-  a->rows = a->dtype == SKIPKV_BF16 && (int64_t)a->max_q * a->group > 16 ? 32 : 16;
-  a->n_rb = (int32_t)(((int64_t)a->max_q * a->group + a->rows - 1) / a->rows);
-  // chunks so that some 1024 workgroups work at a time, of 256 keys at least
-  const int64_t columns = std::max<int64_t>(1, (int64_t)a->batch * a->n_kv_heads * a->n_rb);
-  const int64_t want = std::max<int64_t>(1, 1024 / columns);
-  const int64_t chunk = ((a->max_len + want - 1) / want + 255) / 256 * 256;
-  a->chunk = (int32_t)std::min<int64_t>(std::max<int64_t>(chunk, 256), 1 << 30);
-  a->n_split = std::max(1, (a->max_len + a->chunk - 1) / a->chunk);
-}
-
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
-  const unsigned grid = (unsigned)((int64_t)a.batch * a.n_rb * a.n_split * a.n_kv_heads);
-  if (a.dtype == SKIPKV_F32) hipLaunchKernelGGL((k_attend<SKIPKV_F32, 1, 4>), dim3(grid), dim3(256), 0, st, a);
-  else if (a.rows == 16) hipLaunchKernelGGL((k_attend<SKIPKV_BF16, 1, 4>), dim3(grid), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_attend<SKIPKV_BF16, 2, 4>), dim3(grid), dim3(256), 0, st, a);
-  if (a.n_split > 1) {
-    const unsigned join = (unsigned)(((int64_t)a.total_q * a.n_kv_heads * a.group + 3) / 4);
-    if (a.dtype == SKIPKV_F32) hipLaunchKernelGGL(k_attend_join<SKIPKV_F32>, dim3(join), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_attend_join<SKIPKV_BF16>, dim3(join), dim3(256), 0, st, a);
-  }
+  const dim3 grid(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
+  auto go = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    if (a.hw == 4) hipLaunchKernelGGL((k_attend<DT, 4>), grid, dim3(64 * kWaves), 0, st, a);
+    else if (a.hw == 2) hipLaunchKernelGGL((k_attend<DT, 2>), grid, dim3(64 * kWaves), 0, st, a);
+    else hipLaunchKernelGGL((k_attend<DT, 1>), grid, dim3(64 * kWaves), 0, st, a);
+    if (a.n_split == 1) return;
+    const int64_t rows = a.n_entries * a.hw * a.part_rows;
+    if (a.n_split > 8) hipLaunchKernelGGL((k_attend_join<DT, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_attend_join<DT, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a);
+  };
+  if (a.dtype == SKIPKV_F32) go(std::integral_constant<int, SKIPKV_F32>{});
+  else go(std::integral_constant<int, SKIPKV_BF16>{});
   return hipGetLastError();
 }
 

@@ -355,7 +355,7 @@ hipError_t launch_quant_store(const QuantRowsArgs &a, hipStream_t st);
 hipError_t launch_quant_load(const QuantRowsArgs &a, hipStream_t st);
 
 // Attention of one layer over the 8-bit cache.  Query rows of a (sequence, KV head): row r = j * group + i for query
-// token j and head i of the group, taken in blocks of `rows`; the keys that a block of rows sees are cut into chunks.
+// token j and head i of the group, taken in blocks of `rows`.
 struct AttendArgs {
   const uint8_t *k, *v, *k_exp, *v_exp;  // of the layer
   int64_t stride_head, stride_block, stride_tok;
@@ -367,13 +367,17 @@ struct AttendArgs {
   int64_t q_stride_tok, q_stride_head, out_stride_tok, out_stride_head;
   int32_t dtype, total_q, max_q, max_len;
   float scale;
-  int32_t rows, n_rb;        // query rows per workgroup; blocks of rows per head, at most
-  int32_t chunk, n_split;    // keys per workgroup; chunks per block of rows, at most
-  float *part_o;             // [n_split, total_q, n_q_heads, 128] unnormalised outputs of the chunks
-  float2 *part_ml;           // [n_split, total_q, n_q_heads] (reference, sum), log2 domain
+  // the layout, by plan_attend
+  int32_t rows, n_rb;             // query rows per workgroup; blocks of rows per head, at most
+  int32_t hw;                     // heads side by side in a workgroup
+  int32_t chunk, n_split;         // keys per workgroup; chunks of an entry (sequence, block of rows, group of heads), at most
+  int32_t part_rows;              // rows per chunk's partial results
+  int64_t n_entries;
+  float *part_o;                  // [n_entries, n_split, hw, part_rows, 128] outputs before the division
+  float2 *part_ml;                // [n_entries, n_split, hw, part_rows] (reference, sum), log2 domain
   int32_t *dev_status;
 };
-void plan_attend(AttendArgs *a);  // fills in rows, n_rb, chunk and n_split
+void plan_attend(AttendArgs *a);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st);
 
 struct PagesArgs {
