@@ -452,8 +452,10 @@ void plan_attend(AttendArgs *a) {
     if (a->n_kv_heads % hw) continue;
     const int unit = 32 * kWaves / hw, units = std::max(1, (a->max_len + unit - 1) / unit);
     const int64_t entries = (int64_t)a->batch * a->n_rb * (a->n_kv_heads / hw);
-    for (int per = units; per >= 1; per = std::min(per - 1, per * 7 / 8)) {  // units per workgroup
-      const int split = (units + per - 1) / per;
+    for (int turn = 0; turn <= 4; ++turn) {  // one workgroup per entry, or as many as fill the CUs so many times
+      const int64_t want = turn == 0 ? 1 : std::min<int64_t>(units, 256 * turn / entries);
+      if (want < 1) continue;
+      const int per = (int)((units + want - 1) / want), split = (units + per - 1) / per;  // units per workgroup
       const double turns = (double)((entries * split + 255) / 256);
       const double us = turns * (per * (hw == 4 ? 2.9 : hw == 2 ? 3.05 : 3.3) + 4) + (split > 1 ? 5 : 0);
       if (best == 0 || us < best) {
