@@ -443,10 +443,22 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
 // shortest if all lengths were max_len.  Measured, us, one head / four heads side by side, chunks as the rule has them:
 //   64 x 4 heads, 1152 keys 15.8 / 22.5;  50 x 8 heads, 400-830 keys 18.6 / 22.8;  1 x 8 heads, 4224 keys 11.2 / 12.3;
 //   8 x 8 heads, 32896 keys 127 / 104;  18 x 8 heads, 10 K keys 110 / 74.
+#ifndef ATT_FEW
+#define ATT_FEW 16
+#endif
 void plan_attend(AttendArgs *a) {
   a->rows = 16;
+  if (a->dtype == SKIPKV_BF16 && (int64_t)a->max_q * a->group > ATT_FEW) a->rows = 256;
   a->n_rb = (int32_t)(((int64_t)a->max_q * a->group + a->rows - 1) / a->rows);
   a->part_rows = (int32_t)std::min<int64_t>(a->rows, (int64_t)a->max_q * a->group);
+  if (a->rows > 16) {  // one workgroup per CU
+    a->hw = 1;
+    a->n_entries = (int64_t)a->batch * a->n_rb * a->n_kv_heads;
+    const int64_t want = std::max<int64_t>(1, 256 / a->n_entries);
+    a->chunk = (int32_t)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
+    a->n_split = std::max(1, (a->max_len + a->chunk - 1) / a->chunk);
+    return;
+  }
   double best = 0;
   for (const int hw : {4, 2, 1}) {
     if (a->n_kv_heads % hw) continue;
@@ -473,7 +485,8 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
   const dim3 grid(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
   auto go = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    if (a.hw == 4) hipLaunchKernelGGL((k_attend<DT, 4>), grid, dim3(64 * kWaves), 0, st, a);
+    if (a.rows > 16) (void)launch_attend_rows(a, st);
+    else if (a.hw == 4) hipLaunchKernelGGL((k_attend<DT, 4>), grid, dim3(64 * kWaves), 0, st, a);
     else if (a.hw == 2) hipLaunchKernelGGL((k_attend<DT, 2>), grid, dim3(64 * kWaves), 0, st, a);
     else hipLaunchKernelGGL((k_attend<DT, 1>), grid, dim3(64 * kWaves), 0, st, a);
     if (a.n_split == 1) return;

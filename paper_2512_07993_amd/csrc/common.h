@@ -379,6 +379,7 @@ struct AttendArgs {
 };
 void plan_attend(AttendArgs *a);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st);
+hipError_t launch_attend_rows(const AttendArgs &a, hipStream_t st);
 
 struct PagesArgs {
   int32_t *block_table, *n_held, *free_list, *n_free;
