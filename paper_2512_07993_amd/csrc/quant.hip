@@ -17,18 +17,20 @@ namespace skipkv {
 
 namespace {
 
+constexpr int kLoadAhead = 2;  // positions of a lane that are under way together in a load (64 x 4 heads of 1152 tokens, us, 1 / 2 / 4: 106 / 95 / 102)
+
 // A head's share of the call: positions begin .. end-1 of sequence b, whose first row is seq_off[b].
 struct HeadRange {
   int begin, end, row0;
 };
 // False: nothing to do, or a range that does not fit (reported).
-__device__ __forceinline__ bool head_range(const QuantRowsArgs &a, int lh, int b, HeadRange *out) {
+__device__ __forceinline__ bool head_range(const QuantRowsArgs &a, int lh, int b, bool report, HeadRange *out) {
   const int row0 = a.seq_off[b], room = a.seq_off[b + 1] - row0;
   const int begin = a.begin ? a.begin[(int64_t)lh * a.batch + b] : 0;
   const int64_t end = a.end ? (int64_t)a.end[(int64_t)lh * a.batch + b] : (int64_t)begin + room;
   const int64_t cap = (int64_t)a.table_stride << a.block_log2;
   const bool ok = begin >= 0 && end >= begin && end <= cap && end - begin <= room && row0 >= 0 && (int64_t)row0 + (end - begin) <= a.total_tokens;
-  if (!ok && blockIdx.x == 0 && threadIdx.x == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
+  if (!ok && report && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
   out->begin = begin;
   out->end = (int)end;
   out->row0 = row0;
@@ -50,7 +52,7 @@ __global__ void __launch_bounds__(256) k_quant_store(QuantRowsArgs a) {
   const bool is_v = (int)blockIdx.z >= n_lh;
   const int lh = blockIdx.z - (is_v ? n_lh : 0), l = lh / a.n_kv_heads, h = lh % a.n_kv_heads;
   HeadRange r;
-  if (!head_range(a, lh, b, &r)) return;
+  if (!head_range(a, lh, b, blockIdx.x == 0 && threadIdx.x == 0, &r)) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, team = wave / kWpb, tw = wave % kWpb, piece = lane & 15;
   uint8_t *pool = static_cast<uint8_t *>(is_v ? a.v : a.k) + l * a.stride_layer + h * a.stride_head;
   uint8_t *exps = (is_v ? a.v_exp : a.k_exp) + (int64_t)lh * a.n_blocks;
@@ -143,61 +145,68 @@ __global__ void __launch_bounds__(256) k_quant_store(QuantRowsArgs a) {
   }
 }
 
-// grid = (x, batch, 2 * layers * heads).  Eight lanes per row, 16 codes each.
-template <int DT>
+// grid = (x, batch, 2 * layers * heads / HW).  A lane writes 16 bytes: 16 lanes per bf16 row, 32 per fp32 row.  HW heads side by side,
+// whose rows of a slot are neighbours in memory; kLoadAhead positions of a lane are under way at a time.
+template <int DT, int HW>
 __global__ void __launch_bounds__(256) k_quant_load(QuantRowsArgs a) {
-  constexpr int ESZ = DT == SKIPKV_BF16 ? 2 : 4;
+  constexpr int ESZ = DT == SKIPKV_BF16 ? 2 : 4, kCodes = 16 / ESZ, kLanes = kD / kCodes, kPos = 256 / kLanes / HW, kAhead = kLoadAhead;
   const int n_lh = a.n_layers * a.n_kv_heads, b = blockIdx.y;
-  const bool is_v = (int)blockIdx.z >= n_lh;
-  const int lh = blockIdx.z - (is_v ? n_lh : 0), l = lh / a.n_kv_heads, h = lh % a.n_kv_heads;
+  const bool is_v = (int)blockIdx.z >= n_lh / HW;
+  const int row = threadIdx.x / kLanes, piece = threadIdx.x % kLanes, pos = row / HW;
+  const int lh = (blockIdx.z - (is_v ? n_lh / HW : 0)) * HW + row % HW, l = lh / a.n_kv_heads, h = lh - l * a.n_kv_heads;
   HeadRange r;
-  if (!head_range(a, lh, b, &r)) return;
-  const uint8_t *pool = static_cast<const uint8_t *>(is_v ? a.v : a.k) + l * a.stride_layer + h * a.stride_head;
+  if (!head_range(a, lh, b, blockIdx.x == 0 && pos == 0 && piece == 0, &r)) return;
+  const uint8_t *pool = static_cast<const uint8_t *>(is_v ? a.v : a.k) + l * a.stride_layer + h * a.stride_head + piece * kCodes;
   const uint8_t *exps = (is_v ? a.v_exp : a.k_exp) + (int64_t)lh * a.n_blocks;
-  const int piece = threadIdx.x & 7;
   char *dst = static_cast<char *>(const_cast<void *>(is_v ? a.rv : a.rk)) +
-              (l * a.r_stride_layer + h * a.r_stride_head + (int64_t)r.row0 * a.r_stride_tok) * ESZ + piece * 16 * ESZ;
+              (l * a.r_stride_layer + h * a.r_stride_head + (int64_t)r.row0 * a.r_stride_tok) * ESZ + piece * 16;
   const int32_t *table = a.block_table + (int64_t)b * a.table_stride;
   const int mask = (1 << a.block_log2) - 1;
   bool bad = false;
-  for (int64_t t = r.begin + (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); t < r.end; t += (int64_t)gridDim.x * 32) {
-    const int id = table[t >> a.block_log2];
-    if (id < 0 || id >= a.n_blocks) {
-      bad = true;
-      continue;
+  for (int64_t t0 = r.begin + (int64_t)blockIdx.x * (kAhead * kPos) + pos; t0 < r.end; t0 += (int64_t)gridDim.x * (kAhead * kPos)) {
+    uint32_t w[kAhead][2], e[kAhead];
+    bool in[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t t = t0 + i * kPos;
+      int id = t < r.end ? table[t >> a.block_log2] : -1;
+      in[i] = id >= 0 && id < a.n_blocks;
+      bad |= t < r.end && !in[i];
+      if (in[i]) {
+        const uint8_t *p = pool + (int64_t)id * a.stride_block + (int64_t)((int)t & mask) * a.stride_tok;
+        w[i][0] = *reinterpret_cast<const uint32_t *>(p);
+        if constexpr (kCodes == 8) w[i][1] = *reinterpret_cast<const uint32_t *>(p + 4);
+        e[i] = exps[id];
+      }
     }
-    const uint4 c = *reinterpret_cast<const uint4 *>(pool + (int64_t)id * a.stride_block + (int64_t)((int)t & mask) * a.stride_tok + piece * 16);
-    const float s = scale_of_byte(exps[id]);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    char *o = dst + (t - r.begin) * a.r_stride_tok * ESZ;
-    float x[16];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {  // codes to fp32 first: the product with the scale is the one rounding
-      const uint32_t lo = e4m3_to_bf16x2<false>(w[e], 1.f), hi = e4m3_to_bf16x2<true>(w[e], 1.f);
-      x[4 * e] = __uint_as_float(lo << 16) * s;
-      x[4 * e + 1] = __uint_as_float(lo & 0xFFFF0000u) * s;
-      x[4 * e + 2] = __uint_as_float(hi << 16) * s;
-      x[4 * e + 3] = __uint_as_float(hi & 0xFFFF0000u) * s;
-    }
-    if constexpr (DT == SKIPKV_BF16) {
+    for (int i = 0; i < kAhead; ++i) {
+      if (!in[i]) continue;
+      const float s = scale_of_byte(e[i]);
+      float x[kCodes];
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        reinterpret_cast<uint4 *>(o)[e] = make_uint4(pack_bf16x2(x[8 * e], x[8 * e + 1]), pack_bf16x2(x[8 * e + 2], x[8 * e + 3]),
-                                                     pack_bf16x2(x[8 * e + 4], x[8 * e + 5]), pack_bf16x2(x[8 * e + 6], x[8 * e + 7]));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) reinterpret_cast<float4 *>(o)[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+      for (int k = 0; k < kCodes / 4; ++k) {  // codes to fp32 first: the product with the scale is the one rounding
+        const uint32_t lo = e4m3_to_bf16x2<false>(w[i][k], 1.f), hi = e4m3_to_bf16x2<true>(w[i][k], 1.f);
+        x[4 * k] = __uint_as_float(lo << 16) * s;
+        x[4 * k + 1] = __uint_as_float(lo & 0xFFFF0000u) * s;
+        x[4 * k + 2] = __uint_as_float(hi << 16) * s;
+        x[4 * k + 3] = __uint_as_float(hi & 0xFFFF0000u) * s;
+      }
+      char *o = dst + (t0 + i * kPos - r.begin) * a.r_stride_tok * ESZ;
+      if constexpr (DT == SKIPKV_BF16)
+        *reinterpret_cast<uint4 *>(o) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+      else
+        *reinterpret_cast<float4 *>(o) = make_float4(x[0], x[1], x[2], x[3]);
     }
   }
-  if (__any(bad) && (threadIdx.x & 63) == 0) bad_block(a);
+  if (bad) bad_block(a);
 }
 
-// Workgroups along a sequence: as many as its share of the rows asks for, at least one, some 8192 in all.  They walk the sequence
-// in steps of the grid, so that one sequence may be much longer than the mean.
-unsigned along(const QuantRowsArgs &a, int64_t rows_per_wg) {
-  const int64_t columns = 2ll * a.n_layers * a.n_kv_heads * a.batch;
+// Workgroups along a sequence: as many as its share of the rows asks for, at least one, some `all` in the call.  They walk the
+// sequence in steps of the grid, so that one sequence may be much longer than the mean.
+unsigned along(const QuantRowsArgs &a, int64_t columns, int64_t rows_per_wg, int64_t all) {
   const int64_t longest = (a.total_tokens + rows_per_wg - 1) / rows_per_wg + 1;
-  return (unsigned)std::max<int64_t>(1, std::min(longest, (8192 + columns - 1) / columns));
+  return (unsigned)std::max<int64_t>(1, std::min(longest, (all + columns - 1) / columns));
 }
 
 }  // namespace
@@ -205,7 +214,9 @@ unsigned along(const QuantRowsArgs &a, int64_t rows_per_wg) {
 hipError_t launch_quant_store(const QuantRowsArgs &a, hipStream_t st) {
   auto go = [&](auto dt, auto lbs) {
     constexpr int DT = decltype(dt)::value, LBS = decltype(lbs)::value;
-    const dim3 grid(along(a, std::max(64, 1 << LBS)), a.batch, 2 * a.n_layers * a.n_kv_heads);
+    const int heads = 2 * a.n_layers * a.n_kv_heads;
+    // 16 x 8 heads of 2048-16384 tokens, us, with 2048 / 8192 / 16384 / 32768 workgroups: 253 / 191 / 181 / 179
+    const dim3 grid(along(a, (int64_t)heads * a.batch, std::max(64, 1 << LBS), 32768), a.batch, heads);
     hipLaunchKernelGGL((k_quant_store<DT, LBS>), grid, dim3(256), 0, st, a);
   };
   auto of_size = [&](auto dt) {
@@ -222,9 +233,19 @@ hipError_t launch_quant_store(const QuantRowsArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_quant_load(const QuantRowsArgs &a, hipStream_t st) {
-  const dim3 grid(along(a, 32), a.batch, 2 * a.n_layers * a.n_kv_heads);
-  if (a.dtype == SKIPKV_BF16) hipLaunchKernelGGL(k_quant_load<SKIPKV_BF16>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_quant_load<SKIPKV_F32>, grid, dim3(256), 0, st, a);
+  auto go = [&](auto dt, auto hw) {
+    constexpr int DT = decltype(dt)::value, HW = decltype(hw)::value;
+    const int groups = 2 * a.n_layers * a.n_kv_heads / HW;
+    const dim3 grid(along(a, (int64_t)groups * a.batch, kLoadAhead * 256 / (DT == SKIPKV_BF16 ? 16 : 32) / HW, 16384), a.batch, groups);
+    hipLaunchKernelGGL((k_quant_load<DT, HW>), grid, dim3(256), 0, st, a);
+  };
+  auto of_heads = [&](auto dt) {
+    if (a.n_kv_heads % 4 == 0) go(dt, std::integral_constant<int, 4>{});
+    else if (a.n_kv_heads % 2 == 0) go(dt, std::integral_constant<int, 2>{});
+    else go(dt, std::integral_constant<int, 1>{});
+  };
+  if (a.dtype == SKIPKV_BF16) of_heads(std::integral_constant<int, SKIPKV_BF16>{});
+  else of_heads(std::integral_constant<int, SKIPKV_F32>{});
   return hipGetLastError();
 }
 
