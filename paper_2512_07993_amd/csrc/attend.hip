@@ -443,14 +443,15 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
 // shortest if all lengths were max_len.  Measured, us, one head / four heads side by side, chunks as the rule has them:
 //   64 x 4 heads, 1152 keys 15.8 / 22.5;  50 x 8 heads, 400-830 keys 18.6 / 22.8;  1 x 8 heads, 4224 keys 11.2 / 12.3;
 //   8 x 8 heads, 32896 keys 127 / 104;  18 x 8 heads, 10 K keys 110 / 74.
-#ifndef ATT_FEW
-#define ATT_FEW 16
-#endif
 void plan_attend(AttendArgs *a) {
   a->rows = 16;
-  if (a->dtype == SKIPKV_BF16 && (int64_t)a->max_q * a->group > ATT_FEW) a->rows = 256;
-  a->n_rb = (int32_t)(((int64_t)a->max_q * a->group + a->rows - 1) / a->rows);
-  a->part_rows = (int32_t)std::min<int64_t>(a->rows, (int64_t)a->max_q * a->group);
+  // Two blocks of 16 rows that read the cache one behind the other are faster than a workgroup of 256 rows where the cache is long, us, 21 to 32 rows:
+  // 8 x 8 heads, 32000 keys 123 / 141;  16 x 8 heads, 4200 keys 44 / 48;  64 x 4 heads, 1152 keys 28 / 25.  From 33 rows on it is the
+  // other way round (56 rows: 207 / 145, 65 / 52, 52 / 26).
+  const int64_t rows = (int64_t)a->max_q * a->group;
+  if (a->dtype == SKIPKV_BF16 && (rows > 32 || (rows > 16 && a->max_len <= 2048))) a->rows = 256;
+  a->n_rb = (int32_t)((rows + a->rows - 1) / a->rows);
+  a->part_rows = (int32_t)std::min<int64_t>(a->rows, rows);
   if (a->rows > 16) {  // one workgroup per CU
     a->hw = 1;
     a->n_entries = (int64_t)a->batch * a->n_rb * a->n_kv_heads;
