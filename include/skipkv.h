@@ -542,7 +542,7 @@ typedef struct skipkv_pages {
  * Table entries at and beyond n_held and stack entries at and beyond n_free keep what they held.
  * slot_map[r * total_new + i], for the new token i = new_off[b] .. new_off[b+1]-1 of sequence b, is the slot
  *   block * block_size + (slot in the block) of position len[r, b] + i - new_off[b], where its K and V rows
- *   go; -1 where the sequence does not hold the block.
+ *   go; -1 where the sequence does not hold the block, and for tokens that no sequence has.
  * len       device [n_rows, batch]: lengths before the new tokens; n_rows = 1 for lengths shared by all
  *           heads, n_layers * n_kv_heads for skipkv_ranges.len.
  * new_off   device [batch + 1] CSR of the new tokens, or NULL (none); total_new = host copy of new_off[batch].

@@ -1256,7 +1256,7 @@ int skipkv_pages_workspace_bytes(const skipkv_pages *pages, size_t *out_bytes) {
   if (!out_bytes) return SKIPKV_EINVAL;
   const int rc = check_pages(pages);
   if (rc) return rc;
-  *out_bytes = pages->batch == 0 ? 0 : pages_need_bytes(pages) + align_up(((size_t)pages->batch + 1) * 4);
+  *out_bytes = pages->batch == 0 ? 0 : pages_need_bytes(pages) + align_up(((size_t)pages->batch + 2) * 4);
   return SKIPKV_OK;
 }
 

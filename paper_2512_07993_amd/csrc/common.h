@@ -387,7 +387,7 @@ struct PagesArgs {
   const int32_t *len, *new_off;
   int32_t n_rows, total_new;
   int32_t *slot_map, *dev_status;
-  int32_t *need, *was_held;  // workspace [batch], [batch + 1]: blocks that a sequence needs (-1: leave it alone); blocks held before, then the free ones
+  int32_t *need, *was_held;  // workspace [batch], [batch + 2]: blocks that a sequence needs (-1: leave it alone); blocks held before, then the free ones, then 1 if the state is refused
 };
 hipError_t launch_pages_update(const PagesArgs &a, hipStream_t st);
 

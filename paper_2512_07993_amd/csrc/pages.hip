@@ -3,11 +3,16 @@
 //
 // With P the prefix sums over sequences of the blocks given back, the stack of free blocks after all releases is the old one with
 // entry need_b + i of sequence b's table row at n_free + P_b + i; with G those of the blocks wanted, sequence b's i-th new block is the
-// one at top - 1 - G_b - i, and it is served iff its end G_b + grow_b is at most top.  Every workgroup forms both sums for itself (a few
-// thousand numbers), so that nothing is passed between workgroups: an entry on top of the old stack is read from the
-// table row that gives it back, not from the stack, and rows that give back are not written.  The result does not depend on any order.
+// one at top - 1 - G_b - i, and it is served iff its end G_b + grow_b is at most top.  Every workgroup of the second kernel forms both
+// sums for itself (a few thousand numbers), so that nothing is passed between workgroups: an entry on top of the old stack is read from
+// the table row that gives it back, not from the stack, and rows that give back are not written.  The result does not depend on any
+// order.
 //
-// Bound by the two launches, and by the slots' writes where there are many new tokens.
+// Three kernels: the blocks that every sequence needs, the blocks moved, the slots.  A kernel of its own for the slots reads finished
+// tables; with the slots in the second one, whose workgroups then look up each grown block in the prefix sums, a call takes 17 instead
+// of 13 us (64 sequences, one token, 112 rows) and 53 instead of 34 (256 sequences, 342 tokens each, 256 rows: 90 MB of slots).
+// Bound by the latency of the launches and of their chains of loads (some 12 us), and by the slots' writes where there are many
+// new tokens: 21 us for the 90 MB.
 #include <algorithm>
 
 #include "common.h"
@@ -16,7 +21,7 @@ namespace skipkv {
 
 namespace {
 
-static_assert(SKIPKV_MAX_PAGES_BATCH * 16 <= 64 * 1024, "four numbers per sequence in shared memory");
+static_assert(SKIPKV_MAX_PAGES_BATCH * 12 + 2048 <= 64 * 1024, "three numbers per sequence in shared memory");
 constexpr int kSeqs = 16;  // sequences per workgroup of the first kernel
 
 // Blocks that every sequence needs, and a copy of the counts that the second kernel replaces.
@@ -26,6 +31,7 @@ __global__ void __launch_bounds__(256) k_pages_need(PagesArgs a) {
   int top = 0;
   bool bad = false;
   if (b < a.batch) {
+#pragma unroll 8
     for (int r = group; r < a.n_rows; r += 16) {
       const int n = a.len[(int64_t)r * a.batch + b];
       bad |= n < 0;
@@ -77,14 +83,14 @@ __device__ __forceinline__ longlong2 scan256(longlong2 v, longlong2 (&wave_total
   return v;
 }
 
-// grid = (tokens of the slot map / 256, rows of it / rows_per_wg).  Shared memory: four numbers per sequence.
-__global__ void __launch_bounds__(256) k_pages_move(PagesArgs a, int rows_per_wg) {
+// Blocks given back and taken: table rows, counts and the stack.  Shared memory: three numbers per sequence.
+__global__ void __launch_bounds__(256) k_pages_move(PagesArgs a) {
   extern __shared__ int32_t shared[];
   __shared__ longlong2 wave_total[4];
   __shared__ int any_bad;
-  const int tid = threadIdx.x, n = a.batch, wg = blockIdx.y * gridDim.x + blockIdx.x, n_wg = gridDim.x * gridDim.y;
-  int32_t *const s_held = shared, *const s_need = shared + n;             // before; after (equal where a sequence stays as it is)
-  int32_t *const s_back = shared + 2 * n, *const s_want = shared + 3 * n;  // prefix sums up to and including the sequence: blocks given back, blocks wanted
+  const int tid = threadIdx.x, n = a.batch, wg = blockIdx.x, n_wg = gridDim.x;
+  int32_t *const s_held = shared;                                  // blocks held before
+  int32_t *const s_back = shared + n, *const s_want = shared + 2 * n;  // prefix sums up to and including the sequence: blocks given back, blocks wanted
   const int free0 = a.was_held[n];
   if (tid == 0) any_bad = free0 < 0 || free0 > a.n_blocks;
   __syncthreads();
@@ -99,25 +105,26 @@ __global__ void __launch_bounds__(256) k_pages_move(PagesArgs a, int rows_per_wg
     short_row |= need > a.table_stride;
     if (need < 0 || need > a.table_stride) need = held;
     s_held[b] = held;
-    s_need[b] = need;
-    sums.x += max(held - need, 0);
-    sums.y += max(need - held, 0);
+    s_back[b] = max(held - need, 0);
+    s_want[b] = max(need - held, 0);
+    sums.x += s_back[b];
+    sums.y += s_want[b];
   }
   if (bad) any_bad = 1;  // every writer stores the same value
   longlong2 total;
   const longlong2 upto = scan256(sums, wave_total, &total);  // (its barrier is behind the writes of any_bad)
   const long long total_back = total.x;
-  if (any_bad || free0 + total_back > a.n_blocks) {
-    if (wg == 0 && tid == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_BLOCK_TABLE);
-    if (a.slot_map)
-      for (int64_t i = (int64_t)wg * 256 + tid; i < (int64_t)a.n_rows * a.total_new; i += (int64_t)n_wg * 256) a.slot_map[i] = -1;
-    return;
+  const bool refused = any_bad || free0 + total_back > a.n_blocks;
+  if (wg == 0 && tid == 0) {
+    a.was_held[n + 1] = refused;
+    if (refused && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_BLOCK_TABLE);
   }
+  if (refused) return;
   const int top = free0 + (int)total_back;  // (at most n_blocks)
   long long back = upto.x - sums.x, want = upto.y - sums.y;
   for (int b = lo; b < hi; ++b) {
-    back += max(s_held[b] - s_need[b], 0);
-    want += max(s_need[b] - s_held[b], 0);
+    back += s_back[b];
+    want += s_want[b];
     s_back[b] = (int)back;
     s_want[b] = (int)min(want, (long long)0x7FFFFFFF);
   }
@@ -138,10 +145,13 @@ __global__ void __launch_bounds__(256) k_pages_move(PagesArgs a, int rows_per_wg
   auto at = [&](int pos) -> int32_t {  // entry of the stack after all releases
     if (pos < free0) return a.free_list[pos];
     const int q = pos - free0, b = first_above(s_back, q);
-    return a.block_table[(int64_t)b * a.table_stride + s_need[b] + q - (b > 0 ? s_back[b - 1] : 0)];
+    return a.block_table[(int64_t)b * a.table_stride + s_held[b] - s_back[b] + q];
   };
-  auto grown_at = [&](int b, int i) { return at(top - 1 - (b > 0 ? s_want[b - 1] : 0) - (i - s_held[b])); };
-  auto held_after = [&](int b) { return s_need[b] > s_held[b] && b >= n_served ? s_held[b] : s_need[b]; };
+  auto before = [&](const int32_t *of, int b) { return b > 0 ? of[b - 1] : 0; };
+  auto grown_at = [&](int b, int i) { return at(top - 1 - before(s_want, b) - (i - s_held[b])); };
+  auto held_after = [&](int b) {  // (a sequence that gives back wants none)
+    return s_held[b] - (s_back[b] - before(s_back, b)) + (b < n_served ? s_want[b] - before(s_want, b) : 0);
+  };
   if (wg == 0) {
     if (tid == 0) *a.n_free = left;
     if (a.dev_status && (short_row || (tid == 0 && total.y > taken))) atomicOr(a.dev_status, SKIPKV_DEV_OUT_OF_BLOCKS);
@@ -154,31 +164,59 @@ __global__ void __launch_bounds__(256) k_pages_move(PagesArgs a, int rows_per_wg
   }
   // ---- what stays on the stack of the blocks given back
   for (int i = free0 + wg * 256 + tid; i < left; i += n_wg * 256) a.free_list[i] = at(i);
-  // ---- slots of the new tokens: a thread has one token in several rows
-  const int tok = blockIdx.x * 256 + tid;
-  if (!a.slot_map || tok >= a.total_new) return;
-  int l = 0, h = n;  // the sequence: the last whose first new token is at or before this one
-  while (h - l > 1) {
-    const int mid = (l + h) / 2;
-    if (a.new_off[mid] <= tok) l = mid;
-    else h = mid;
+}
+
+// Slots of the new tokens, from the tables as they are now.  grid = (tokens / 256, rows / rows_per_wg): a thread has one token in
+// several rows.
+__global__ void __launch_bounds__(256) k_pages_slots(PagesArgs a, int rows_per_wg, uint32_t div_mul, int div_shift) {
+  __shared__ int wave_seq[4];
+  __shared__ int32_t s_seq[256];  // a sequence whose tokens begin here (plus one), 0: none does
+  const int tid = threadIdx.x, n = a.batch, tok0 = blockIdx.x * 256, tok = tok0 + tid;
+  const bool refused = a.was_held[n + 1] != 0;
+  s_seq[tid] = 0;
+  __syncthreads();
+  for (int b = tid; b < n; b += 256) {
+    const int first = a.new_off[b], end = a.new_off[b + 1], need = a.need[b];
+    if (need >= 0 && first < end && first < tok0 + 256ll && end > tok0) atomicMax(&s_seq[max(first, tok0) - tok0], b + 1);
   }
-  const int ahead = tok - a.new_off[l], now = held_after(l), was = s_held[l];
-  const bool known = a.need[l] >= 0 && ahead >= 0;
+  __syncthreads();
+  // the sequence of the thread's token: the last one that begins at or before it
+  int seq = s_seq[tid];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int x = __shfl_up(seq, d);
+    if ((tid & 63) >= d) seq = max(seq, x);
+  }
+  if ((tid & 63) == 63) wave_seq[tid >> 6] = seq;
+  __syncthreads();
+  for (int w = 0; w < (tid >> 6); ++w) seq = max(seq, wave_seq[w]);
+  if (tok >= a.total_new) return;
+  const int l = max(seq - 1, 0);
+  const int64_t ahead = (int64_t)tok - a.new_off[l];
+  const bool known = seq > 0 && !refused && ahead >= 0 && ahead <= 0x7FFFFFFF && tok < a.new_off[l + 1];
+  const int held = known ? a.n_held[l] : 0;
   const int32_t *row = a.block_table + (int64_t)l * a.table_stride;
+  // eight rows at a time: their lengths, then their entries of the table, then the slots, so that the loads overlap
+  constexpr int kRows = 8;
   const int r1 = min((int)(blockIdx.y + 1) * rows_per_wg, a.n_rows);
-#pragma unroll 4
-  for (int r = blockIdx.y * rows_per_wg; r < r1; ++r) {
-    const int64_t pos = (int64_t)a.len[(int64_t)r * n + l] + ahead;
-    int32_t slot = -1;
-    if (known && pos >= 0 && pos <= 0x7FFFFFFF) {
-      const uint32_t bi = (uint32_t)pos / (uint32_t)a.block_size;
-      if (bi < (uint32_t)now) {
-        const int32_t id = bi < (uint32_t)was ? row[bi] : grown_at(l, (int)bi);
-        slot = (int32_t)((uint32_t)id * (uint32_t)a.block_size + ((uint32_t)pos - bi * (uint32_t)a.block_size));
-      }
+  for (int r0 = blockIdx.y * rows_per_wg; r0 < r1; r0 += kRows) {
+    uint32_t pos[kRows], bi[kRows];
+    int32_t id[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int len = (a.len + (int64_t)min(r0 + i, r1 - 1) * n)[l];
+      pos[i] = len >= 0 && known ? (uint32_t)len + (uint32_t)ahead : 0xFFFFFFFFu;
     }
-    a.slot_map[(int64_t)r * a.total_new + tok] = slot;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      bi[i] = pos[i] <= 0x7FFFFFFFu ? __umulhi(pos[i] * 2, div_mul) >> div_shift : 0xFFFFFFFFu;
+      id[i] = bi[i] < (uint32_t)held ? row[bi[i]] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const uint32_t slot = (uint32_t)id[i] * (uint32_t)a.block_size + (pos[i] - bi[i] * (uint32_t)a.block_size);
+      if (r0 + i < r1) (a.slot_map + (int64_t)(r0 + i) * a.total_new)[tok] = bi[i] < (uint32_t)held ? (int32_t)slot : -1;
+    }
   }
 }
 
@@ -186,16 +224,18 @@ __global__ void __launch_bounds__(256) k_pages_move(PagesArgs a, int rows_per_wg
 
 hipError_t launch_pages_update(const PagesArgs &a, hipStream_t st) {
   hipLaunchKernelGGL(k_pages_need, dim3((a.batch + kSeqs - 1) / kSeqs), dim3(256), 0, st, a);
-  // a thread per new token and 8 rows of the slot map, or as many rows as leave some 2048 workgroups; without a slot map a
-  // workgroup per 16 sequences
-  unsigned x = (unsigned)std::max(1, std::min(256, a.batch / 16)), y = 1;
-  int rows = 1;
-  if (a.slot_map) {
-    x = (unsigned)((a.total_new + 255) / 256);
-    rows = (int)std::max<int64_t>(8, ((int64_t)a.n_rows * x + 2047) / 2048);
-    y = (unsigned)((a.n_rows + rows - 1) / rows);
-  }
-  hipLaunchKernelGGL(k_pages_move, dim3(x, y), dim3(256), (size_t)a.batch * 16, st, a, rows);
+  // four sequences to a workgroup, a wave to each
+  hipLaunchKernelGGL(k_pages_move, dim3(std::max(1, std::min(256, a.batch / 4))), dim3(256), (size_t)a.batch * 12, st, a);
+  if (!a.slot_map) return hipGetLastError();
+  // pos / d for pos < 2^31 as pos * m >> 31 + s, with 2^s >= d and m = 2^(31 + s) / d rounded up, e = m d - 2^(31 + s) < 2^s: the
+  // product is above the quotient by pos e / (2^(31 + s) d) < 1 / d
+  int div_shift = 0;
+  while ((1ll << div_shift) < a.block_size) ++div_shift;
+  const uint32_t div_mul = (uint32_t)(((1ull << (31 + div_shift)) + a.block_size - 1) / a.block_size);
+  // eight rows to a thread, or a multiple of eight that leaves some 2048 workgroups
+  const unsigned x = (unsigned)((a.total_new + 255ll) / 256);
+  const int rows = (int)std::max<int64_t>(1, ((int64_t)a.n_rows * x + 2048 * 8 - 1) / (2048 * 8)) * 8;
+  hipLaunchKernelGGL(k_pages_slots, dim3(x, (unsigned)((a.n_rows + rows - 1) / rows)), dim3(256), 0, st, a, rows, div_mul, div_shift);
   return hipGetLastError();
 }
 

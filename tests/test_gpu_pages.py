@@ -196,3 +196,39 @@ def test_without_a_slot_map_or_new_tokens():
     want = plain(*state, 16, np.array([[10, 50]]), [0, 0])
     np.testing.assert_array_equal(pg.block_table.cpu().numpy(), want[0])
     assert pg.n_held.tolist() == [1, 4] and int(pg.n_free.item()) == want[3]
+
+
+@pytest.mark.parametrize("bs", [1, 3, 7, 16, 100, 128, 1000])
+def test_many_new_tokens_at_every_block_size(bs):
+    """Tokens of a sequence that span several workgroups, empty sequences between them, blocks of sizes that no shift divides."""
+    rng = np.random.default_rng(30 + bs)
+    batch, rows = 9, 11
+    lens = rng.integers(0, 700, (rows, batch))
+    lens[:, 3] = 0
+    counts = [1, 0, 700, 257, 0, 0, 255, 1, 300]
+    need = [-(-(int(lens[:, b].max()) + counts[b]) // bs) for b in range(batch)]
+    held = [max(0, need[b] + (-1) ** b * int(rng.integers(0, 5))) for b in range(batch)]
+    state = _state(rng, batch, max(need) + 5, held, 40)
+    _check(state, bs, lens, counts)
+
+
+def test_more_rows_than_a_thread_takes_at_a_time():
+    rng = np.random.default_rng(31)
+    state = _state(rng, 300, 6, rng.integers(0, 7, 300), 700)
+    lens = rng.integers(0, 80, (97, 300))
+    _check(state, 16, lens, [int(x) for x in rng.integers(0, 4, 300)])
+
+
+def test_offsets_below_zero_and_tokens_of_nobody():
+    """A first offset below zero and a total beyond the last offset: slots of -1 and nothing else."""
+    rng = np.random.default_rng(32)
+    table, held, free, n_free = _state(rng, 2, 8, [2, 2], 9)
+    pg = B.Pages(_cuda(table), _cuda(held), _cuda(free), _cuda(np.array([n_free], dtype=np.int32)), 16)
+    off = torch.tensor([-2 ** 31, 2, 4], dtype=torch.int32, device="cuda")
+    slots = torch.full((1, 6), -7, dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    B.skipkv_pages_update(pg, torch.tensor([[20, 20]], dtype=torch.int32, device="cuda"), off, 6, slots, ws, status)
+    t = pg.block_table.cpu().numpy()
+    assert slots.tolist() == [[-1, -1, int(t[1, 1]) * 16 + 4, int(t[1, 1]) * 16 + 5, -1, -1]]
+    assert pg.n_held.tolist() == [2, 2] and int(status.item()) == B.DEV_OUT_OF_BLOCKS
