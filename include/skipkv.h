@@ -566,7 +566,7 @@ int skipkv_pages_update(const skipkv_pages *pages, const int32_t *len, int32_t n
  * Scales being powers of two, a stored value is a bf16 number (but for values below 2^-133), and it stays
  * the same number when it is loaded, moved to another block and stored again, unless it falls
  * among the subnormals there (below 2^-6 of the new scale).
- * Strides are in elements (= bytes) and multiples of 16; element (l, h, block p, slot s, d) at
+ * A table row spans at most 2^30 slots.  Strides are in elements (= bytes) and multiples of 16; element (l, h, block p, slot s, d) at
  * l * stride_layer + h * stride_head + p * stride_block + s * stride_tok + d.  Lengths are per head like skipkv_ranges.len.
  */
 typedef struct skipkv_quant_cache {
@@ -635,7 +635,9 @@ typedef struct skipkv_queries {
  * A query that sees no key (N < m_b: its position is negative) gets out = 0, lse = -inf.  Slots beyond N and keys that
  * a query does not see have no influence on it, whatever they hold.
  * len   device [n_kv_heads, batch]: this layer's lengths, the query tokens included.
- * The result does not depend on max_len and max_q but for the order of additions.  A length that is negative, above
+ * fp32 queries enter as three bf16 parts and fp32 weights of the softmax as three, those of bf16 queries as two, or as one where a
+ * KV head has more than 16 (from 2048 slots on 32) rows max_q * n_q_heads / n_kv_heads.  But for that and the order of
+ * additions the result does not depend on max_len and max_q.  A length that is negative, above
  * max_len or above table_stride * block_size (SKIPKV_DEV_BAD_LENGTHS), or a block id outside [0, n_blocks) among a head's
  * blocks (SKIPKV_DEV_BAD_BLOCK_TABLE), makes the rows concerned NaN; a sequence whose q_off entries
  * descend, leave [0, total_q] or are more than max_q apart gets no output (SKIPKV_DEV_BAD_LENGTHS).

@@ -183,6 +183,21 @@ def _stream(stream) -> Optional[int]:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _ints(t, device: int, optional=False) -> Optional[int]:
+    """Address of a contiguous int32 tensor that lies on `device` (an index, -1: the host)."""
+    if t is None and optional:
+        return None
+    assert t.dtype == torch.int32 and t.is_contiguous() and t.get_device() == device
+    return t.data_ptr()
+
+
+def _here(t) -> int:
+    """Device of a tensor, which has to be the current one: a launch goes there."""
+    device = t.get_device()
+    assert device < 0 or device == torch._C._cuda_getDevice(), "the tensors are on another device than the current one"
+    return device
+
+
 def dtype_code(t: torch.dtype) -> int:
     if t == torch.float32:
         return F32
@@ -505,12 +520,11 @@ class Pages:
     block_size: int
 
     def c(self) -> CPages:
-        bt = self.block_table
+        bt, device = self.block_table, self.block_table.get_device()
         assert bt.dim() == 2 and bt.shape[0] == self.n_held.numel() and (bt.stride(1) == 1 or bt.shape[1] <= 1)
-        assert all(t.dtype == torch.int32 for t in (bt, self.n_held, self.free_list, self.n_free))
-        assert self.n_held.is_contiguous() and self.free_list.is_contiguous()
-        return CPages(bt.data_ptr(), _ptr(self.n_held), _ptr(self.free_list), _ptr(self.n_free), bt.shape[0], bt.stride(0),
-                      self.block_size, self.free_list.numel())
+        assert bt.dtype == torch.int32 and self.n_free.numel() >= 1
+        return CPages(bt.data_ptr(), _ints(self.n_held, device), _ints(self.free_list, device), _ints(self.n_free, device),
+                      bt.shape[0], bt.stride(0), self.block_size, self.free_list.numel())
 
 
 def skipkv_pages_workspace_bytes(pages: Pages) -> int:
@@ -521,11 +535,12 @@ def skipkv_pages_workspace_bytes(pages: Pages) -> int:
 
 def skipkv_pages_update(pages: Pages, len, new_off, total_new: int, slot_map, ws, dev_status=None, stream=None) -> None:
     """len: [n_rows, B] (or [L, Hk, B]: n_rows = L * Hk); new_off: [B + 1] or None; slot_map: [n_rows, total_new] or None."""
-    assert len.is_contiguous() and len.dtype == torch.int32 and len.shape[-1] == pages.n_held.numel()
-    n_rows = len.numel() // max(len.shape[-1], 1) if len.numel() else 1
-    assert slot_map is None or (slot_map.is_contiguous() and slot_map.dtype == torch.int32 and slot_map.numel() == n_rows * total_new)
-    _check(lib().skipkv_pages_update(C.byref(pages.c()), _ptr(len), n_rows, _ptr(new_off), total_new, _ptr(slot_map),
-                                     _ptr(dev_status), _ptr(ws), _nbytes(ws), _stream(stream)))
+    device, batch = _here(pages.block_table), pages.n_held.numel()
+    assert len.shape[-1] == batch and (new_off is None or new_off.numel() == batch + 1)
+    n_rows = len.numel() // max(batch, 1) if len.numel() else 1
+    assert slot_map is None or slot_map.numel() == n_rows * total_new
+    _check(lib().skipkv_pages_update(C.byref(pages.c()), _ints(len, device), n_rows, _ints(new_off, device, True), total_new,
+                                     _ints(slot_map, device, True), _ptr(dev_status), _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
 @dataclass
@@ -539,15 +554,19 @@ class QuantCache:
     block_table: torch.Tensor
 
     def c(self) -> CQuantCache:
-        k, bt = self.k, self.block_table
-        assert k.dim() == 5 and k.element_size() == 1 and k.stride(4) == 1 and self.v.stride() == k.stride() and self.v.shape == k.shape
-        assert self.v.element_size() == 1
-        for e in (self.k_exp, self.v_exp):
-            assert e.dtype == torch.uint8 and e.is_contiguous() and e.shape == (k.shape[0], k.shape[3], k.shape[1])
-        assert bt.dim() == 2 and bt.dtype == torch.int32 and (bt.stride(1) == 1 or bt.shape[1] <= 1)
-        return CQuantCache(_ptr(k), _ptr(self.v), _ptr(self.k_exp), _ptr(self.v_exp), k.stride(0), k.stride(3), k.stride(1),
-                           k.stride(2), k.shape[0], k.shape[3], k.shape[4], bt.shape[0], k.shape[2], k.shape[1], bt.stride(0),
-                           _ptr(bt))
+        # Strides and shapes once each: a look at a tensor's stride or size costs 0.2 us, and a call for one
+        # token spends longer here than on the GPU (this structure 17.8 -> 9.6 us).
+        k, v, ke, ve, bt = self.k, self.v, self.k_exp, self.v_exp, self.block_table
+        st, sh, bst = k.stride(), tuple(k.shape), bt.stride()
+        assert len(sh) == 5 and st[4] == 1 and k.element_size() == 1 and v.stride() == st and v.shape == sh and v.element_size() == 1
+        L, blocks, slots, heads, dim = sh
+        exps, device = (L, heads, blocks), k.get_device()
+        assert v.get_device() == ke.get_device() == ve.get_device() == bt.get_device() == device
+        assert ke.dtype == ve.dtype == torch.uint8 and ke.is_contiguous() and ve.is_contiguous() and ke.shape == exps and ve.shape == exps
+        batch, wide = bt.shape
+        assert bt.dtype == torch.int32 and (bst[1] == 1 or wide <= 1)
+        return CQuantCache(k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), st[0], st[3], st[1], st[2], L, heads, dim,
+                           batch, slots, blocks, bst[0], bt.data_ptr())
 
 
 @dataclass
@@ -562,21 +581,30 @@ class Queries:
     lse: Optional[torch.Tensor] = None
 
     def c(self) -> CQueries:
-        q, o = self.q, self.out
-        assert q.dim() == 3 and o.shape == q.shape and o.dtype == q.dtype and q.stride(2) == 1 and o.stride(2) == 1
-        assert self.lse is None or (self.lse.is_contiguous() and self.lse.dtype == torch.float32 and self.lse.shape == q.shape[:2])
-        return CQueries(_ptr(q), _ptr(o), _ptr(self.lse), q.stride(0), q.stride(1), o.stride(0), o.stride(1), dtype_code(q.dtype),
-                        q.shape[1], q.shape[0], self.max_q, self.max_len, self.scale, _ptr(self.q_off))
+        q, o, lse = self.q, self.out, self.lse
+        qs, os_, sh = q.stride(), o.stride(), tuple(q.shape)
+        assert len(sh) == 3 and o.shape == sh and o.get_device() == q.get_device() and o.dtype == q.dtype and qs[2] == 1 and os_[2] == 1
+        assert lse is None or (lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == sh[:2]
+                               and lse.get_device() == q.get_device())
+        return CQueries(q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), qs[0], qs[1], os_[0], os_[1],
+                        dtype_code(q.dtype), sh[1], sh[0], self.max_q, self.max_len, self.scale, _ints(self.q_off, q.get_device()))
+
+
+def _quant_rows(call, qc: QuantCache, rows: Cache, first_layer: int, begin, end, dev_status, stream) -> None:
+    device = _here(qc.k)
+    assert rows.k.get_device() == device
+    for t in (begin, end):
+        assert t is None or t.numel() == rows.k.shape[0] * qc.k.shape[3] * qc.block_table.shape[0]
+    _check(call(C.byref(qc.c()), C.byref(rows.c()), first_layer, _ints(begin, device, True), _ints(end, device, True),
+                _ptr(dev_status), _stream(stream)))
 
 
 def skipkv_quant_store(qc: QuantCache, rows: Cache, first_layer: int, begin, end, dev_status=None, stream=None) -> None:
-    _check(lib().skipkv_quant_store(C.byref(qc.c()), C.byref(rows.c()), first_layer, _ptr(begin), _ptr(end), _ptr(dev_status),
-                                    _stream(stream)))
+    _quant_rows(lib().skipkv_quant_store, qc, rows, first_layer, begin, end, dev_status, stream)
 
 
 def skipkv_quant_load(qc: QuantCache, rows: Cache, first_layer: int, begin, end, dev_status=None, stream=None) -> None:
-    _check(lib().skipkv_quant_load(C.byref(qc.c()), C.byref(rows.c()), first_layer, _ptr(begin), _ptr(end), _ptr(dev_status),
-                                   _stream(stream)))
+    _quant_rows(lib().skipkv_quant_load, qc, rows, first_layer, begin, end, dev_status, stream)
 
 
 def skipkv_quant_attend_workspace_bytes(qc: QuantCache, queries: Queries) -> int:
@@ -586,8 +614,10 @@ def skipkv_quant_attend_workspace_bytes(qc: QuantCache, queries: Queries) -> int
 
 
 def skipkv_quant_attend(qc: QuantCache, layer: int, queries: Queries, len, ws, dev_status=None, stream=None) -> None:
-    assert len.is_contiguous() and len.dtype == torch.int32 and len.shape == (qc.k.shape[3], qc.block_table.shape[0])
-    _check(lib().skipkv_quant_attend(C.byref(qc.c()), layer, C.byref(queries.c()), _ptr(len), _ptr(dev_status), _ptr(ws),
+    device = _here(qc.k)
+    assert len.shape == (qc.k.shape[3], qc.block_table.shape[0]) and queries.q.get_device() == device
+    assert queries.q_off.numel() == len.shape[1] + 1
+    _check(lib().skipkv_quant_attend(C.byref(qc.c()), layer, C.byref(queries.c()), _ints(len, device), _ptr(dev_status), _ptr(ws),
                                      _nbytes(ws), _stream(stream)))
 
 

@@ -1,0 +1,238 @@
+"""The 8-bit cache and its attention where the kernels change their way: heads taken together, keys cut into chunks and
+joined, blocks of 16 and of 256 query rows; in graphs, on two streams, with blocks that sequences share; and what the binding
+refuses."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2512_07993_amd import binding as B
+
+from quant_helpers import Pool, on_device
+from test_gpu_quant_attend import SCALE, _cuda, build, check, parts_of, queries, run
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+@pytest.mark.parametrize("heads", [1, 2, 3, 4, 6, 8, 12])
+@pytest.mark.parametrize("dtype,m,group", [("bf16", 1, 4), ("f32", 2, 3)])
+def test_heads_of_different_length_in_cut_caches(heads, dtype, m, group):
+    """Heads that a workgroup takes together end in different chunks; some have nothing in the later ones, some nothing at all."""
+    rng = np.random.default_rng(100 + heads)
+    lens = rng.integers(0, 5000, (heads, 2))
+    lens[0, 0], lens[-1, 1] = 4999, 0
+    lens[heads // 2, 0] = 1
+    k, v, table = build(rng, heads, lens[None], 16)
+    q = queries(rng, 2 * m, heads * group, dtype)
+    out, lse, status = run(on_device(k, v, table), 0, q, [m, m], lens, dtype, max_len=5000)
+    assert status == 0
+    check(out, lse, q, [m, m], lens, k, v, table, 16, 0, parts_of(dtype, m, group))
+
+
+@pytest.mark.parametrize("layout", ["slots", "heads"])
+@pytest.mark.parametrize("batch,heads", [(1, 4), (40, 4), (3, 2)])
+def test_one_and_many_sequences_in_both_layouts(layout, batch, heads):
+    rng = np.random.default_rng(200 + batch)
+    lens = rng.integers(1, 1200, (heads, batch))
+    k, v, table = build(rng, heads, lens[None], 64)
+    q = queries(rng, batch, heads * 4, "bf16")
+    out, lse, status = run(on_device(k, v, table, heads_before_slots=layout == "heads"), 0, q, [1] * batch, lens, "bf16")
+    assert status == 0
+    check(out, lse, q, [1] * batch, lens, k, v, table, 64, 0, parts_of("bf16", 1, 4))
+
+
+@pytest.mark.parametrize("longest", [2040, 2500, 6100])
+@pytest.mark.parametrize("m,group", [(4, 4), (5, 4), (8, 4), (9, 4), (17, 1), (32, 1), (33, 1), (4, 8), (3, 7)])
+def test_rows_around_the_change_of_kernel(m, group, longest):
+    """16 and 17, 32 and 33 rows, below and above 2048 slots; the other sequence has fewer rows and keys."""
+    rng = np.random.default_rng(300 + m)
+    lens = np.array([[longest, 40], [longest // 3, 2]])
+    k, v, table = build(rng, 2, lens[None], 32)
+    ms = [m, 2]
+    q = queries(rng, m + 2, 2 * group, "bf16")
+    out, lse, status = run(on_device(k, v, table), 0, q, ms, lens, "bf16")
+    assert status == 0
+    check(out, lse, q, ms, lens, k, v, table, 32, 0, parts_of("bf16", m, group))
+
+
+def test_many_rows_over_a_long_cache():
+    """Two blocks of 256 rows, keys cut and joined, one head shorter than the queries."""
+    rng = np.random.default_rng(400)
+    lens = np.array([[9000], [130], [60]])
+    k, v, table = build(rng, 3, lens[None], 128)
+    q = queries(rng, 100, 12, "bf16")
+    out, lse, status = run(on_device(k, v, table), 0, q, [100], lens, "bf16")
+    assert status == 0
+    check(out, lse, q, [100], lens, k, v, table, 128, 0, parts_of("bf16", 100, 4))
+    assert bool((out[:40, 8:] == 0).all()) and bool((lse[:40, 8:] == -np.inf).all())
+
+
+def test_many_rows_with_lengths_and_blocks_that_do_not_fit():
+    rng = np.random.default_rng(401)
+    lens = np.array([[700, 300, 520], [80, 310, 90]])
+    k, v, table = build(rng, 2, lens[None], 16)
+    ms = [70, 66, 80]
+    q = queries(rng, sum(ms), 8, "bf16")
+    clean, _, _ = run(on_device(k, v, table), 0, q, ms, lens, "bf16")
+    bad, t2 = lens.copy(), table.copy()
+    bad[1, 0] = 701
+    t2[2, 20] = k.codes.shape[1]                              # the first block id that does not exist; beyond head 1's keys
+    out, lse, status = run(on_device(k, v, t2), 0, q, ms, bad, "bf16", max_len=700)
+    assert status == B.DEV_BAD_LENGTHS | B.DEV_BAD_BLOCK_TABLE
+    gone = torch.zeros(sum(ms), 8, dtype=torch.bool, device="cuda")
+    gone[:70, 4:] = True
+    gone[136:, :4] = True
+    assert bool(torch.isnan(out[gone]).all()) and bool(torch.isnan(lse[gone]).all()) and torch.equal(out[~gone], clean[~gone])
+
+
+@pytest.mark.parametrize("m", [1, 5, 90])
+def test_in_a_graph_with_inputs_that_change(m):
+    """Store, load and attention of one step, captured once and replayed with other lengths, rows and queries; eager work of the
+    same kind in between."""
+    rng = np.random.default_rng(500 + m)
+    bs, heads, batch, cap = 16, 4, 3, 3200
+    width = cap // bs
+    table = rng.permutation(batch * width).reshape(batch, width).astype(np.int32)
+    pools = [Pool(1, batch * width, bs, heads) for _ in range(2)]
+    qc = on_device(*pools, table)
+    off = _cuda(np.arange(batch + 1, dtype=np.int32) * m)
+    full = _cuda(np.arange(batch + 1, dtype=np.int32) * cap)
+    new = [torch.zeros((1, heads, batch * m, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    back = [torch.zeros((1, heads, batch * cap, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    rows = B.Cache(new[0], new[1], heads * 4, off, off, off, batch * m, 0)
+    whole = B.Cache(back[0], back[1], heads * 4, full, full, full, batch * cap, 0)
+    begin, end = (torch.zeros((1, heads, batch), dtype=torch.int32, device="cuda") for _ in range(2))
+    q = torch.zeros((batch * m, heads * 4, D), dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(q)
+    qs = B.Queries(q, out, off, max_q=m, max_len=cap, scale=SCALE)
+    ws = torch.empty(B.skipkv_quant_attend_workspace_bytes(qc, qs) + 256, dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        B.skipkv_quant_store(qc, rows, 0, begin, end, None, stream)
+        B.skipkv_quant_attend(qc, 0, qs, end[0], ws, None, stream)
+        B.skipkv_quant_load(qc, whole, 0, None, end, None, stream)
+
+    def inputs(i):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        for t in new + [q]:
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        n = torch.from_numpy(rng.integers(0, cap - m + 1, (1, heads, batch)).astype(np.int32))
+        begin.copy_(n)
+        end.copy_(n + m)
+        for t in (qc.k, qc.v):                                 # finite codes of either sign
+            t.copy_(torch.randint(0, 127, t.shape, generator=g, device="cuda", dtype=torch.uint8) + 128 * torch.randint(0, 2, t.shape, generator=g, device="cuda", dtype=torch.uint8))
+        for t in (qc.k_exp, qc.v_exp):
+            t.fill_(120)
+        for t in back:
+            t.zero_()
+        out.zero_()
+
+    inputs(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(1, 5):
+        state = rng.bit_generator.state
+        inputs(i)
+        step()
+        want = [t.clone() for t in (out, *back, qc.k, qc.v, qc.k_exp, qc.v_exp)]
+        rng.bit_generator.state = state
+        inputs(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, (out, *back, qc.k, qc.v, qc.k_exp, qc.v_exp)):
+            assert torch.equal(a, b)
+        assert bool(torch.isfinite(out).all()) and float(out.abs().max()) > 0
+
+
+def test_two_calls_at_once_on_two_streams():
+    rng = np.random.default_rng(600)
+    lens = rng.integers(1, 3000, (4, 6))
+    k, v, table = build(rng, 4, lens[None], 16)
+    qc = on_device(k, v, table)
+    cases = []
+    for dtype, m in (("bf16", 1), ("bf16", 60), ("f32", 2)):
+        ms, q = [m] * 6, queries(rng, 6 * m, 16, dtype)
+        want, _, _ = run(qc, 0, q, ms, lens, dtype)
+        out = torch.zeros_like(q)
+        off = _cuda(np.arange(7, dtype=np.int32) * m)
+        qs = B.Queries(q, out, off, max_q=m, max_len=int(lens.max()), scale=SCALE)
+        ws = torch.empty(B.skipkv_quant_attend_workspace_bytes(qc, qs) + 256, dtype=torch.uint8, device="cuda")
+        cases.append((qs, ws, want, torch.cuda.Stream()))
+    n = _cuda(lens.astype(np.int32))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for qs, ws, _, st in cases:
+            B.skipkv_quant_attend(qc, 0, qs, n, ws, None, st)
+    torch.cuda.synchronize()
+    for qs, _, want, _ in cases:
+        assert torch.equal(qs.out, want)
+
+
+def test_sequences_that_share_blocks():
+    """A common beginning held once: the same ids in two table rows, and one sequence twice in the batch."""
+    rng = np.random.default_rng(700)
+    lens = np.array([[200, 150, 200]])
+    k, v, table = build(rng, 1, lens[None], 16)
+    table[1, :5] = table[0, :5]
+    table[2] = table[0]
+    q = queries(rng, 3, 4, "bf16")
+    q[2] = q[0]
+    qc = on_device(k, v, table)
+    out, lse, status = run(qc, 0, q, [1, 1, 1], lens, "bf16")
+    assert status == 0 and torch.equal(out[2], out[0])
+    check(out, lse, q, [1, 1, 1], lens, k, v, table, 16, 0, parts_of("bf16", 1, 4))
+    off = _cuda(np.array([0, 200, 350, 550], dtype=np.int32))
+    back = [torch.zeros((1, 1, 550, D), device="cuda") for _ in range(2)]
+    B.skipkv_quant_load(qc, B.Cache(back[0], back[1], 4, off, off, off, 550, 0), 0, None, _cuda(lens[None].astype(np.int32)))
+    for pool, t in ((k, back[0]), (v, back[1])):
+        for b, at in enumerate((0, 200, 350)):
+            n = int(lens[0, b])
+            np.testing.assert_array_equal(t[0, 0, at:at + n].double().cpu().numpy(), pool.rows(0, 0, table[b], 16, n))
+
+
+def test_what_the_binding_refuses(monkeypatch):
+    rng = np.random.default_rng(800)
+    lens = np.array([[20, 30]])
+    k, v, table = build(rng, 1, lens[None], 16)
+    qc = on_device(k, v, table)
+    q = queries(rng, 2, 4, "bf16")
+    off = _cuda(np.array([0, 1, 2], dtype=np.int32))
+    n = _cuda(lens.astype(np.int32))
+    qs = B.Queries(q, torch.zeros_like(q), off, max_q=1, max_len=30, scale=SCALE)
+    rows = B.Cache(*(torch.zeros((1, 1, 2, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)), 4, off, off, off, 2, 0)
+    pages = B.Pages(qc.block_table, _cuda(np.array([2, 2], dtype=np.int32)), torch.zeros(9, dtype=torch.int32, device="cuda"),
+                    torch.zeros(1, dtype=torch.int32, device="cuda"), 16)
+    ws = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    for bad in (n.long(), n.cpu(), n[:, :1], torch.stack([n, n], 2)[:, :, 0]):
+        with pytest.raises(AssertionError):
+            B.skipkv_quant_attend(qc, 0, qs, bad, ws)
+    for bad in (n[None].long(), n[None].cpu(), n[None, :, :1]):
+        for call in (B.skipkv_quant_store, B.skipkv_quant_load):
+            with pytest.raises(AssertionError):
+                call(qc, rows, 0, bad, None)
+            with pytest.raises(AssertionError):
+                call(qc, rows, 0, None, bad)
+    for bad in (dict(q_off=off.long()), dict(q_off=off.cpu()), dict(q_off=off[:2]), dict(out=torch.zeros_like(q).float()), dict(out=qs.out.cpu()),
+                dict(lse=torch.zeros(2, 3, device="cuda"))):
+        d = dict(q=q, out=qs.out, q_off=off, max_q=1, max_len=30, scale=SCALE)
+        with pytest.raises(AssertionError):
+            B.skipkv_quant_attend(qc, 0, B.Queries(**dict(d, **bad)), n, ws)
+    with pytest.raises(AssertionError):
+        B.skipkv_pages_update(pages, n.long(), off, 2, None, ws)
+    with pytest.raises(AssertionError):
+        B.skipkv_pages_update(pages, n, off, 2, torch.zeros(3, dtype=torch.int32, device="cuda"), ws)
+    with pytest.raises(AssertionError):
+        B.skipkv_pages_update(pages, n, off[:2], 1, None, ws)
+    with pytest.raises(B.SkipKVError):
+        B.skipkv_pages_update(pages, n, off, 2, None, ws[:16])
+    # another current device than the tensors'
+    here = torch._C._cuda_getDevice()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: here + 1)
+    for call in (lambda: B.skipkv_quant_attend(qc, 0, qs, n, ws), lambda: B.skipkv_quant_store(qc, rows, 0, None, None),
+                 lambda: B.skipkv_quant_load(qc, rows, 0, None, None), lambda: B.skipkv_pages_update(pages, n, off, 2, None, ws)):
+        with pytest.raises(AssertionError, match="another device"):
+            call()
