@@ -142,7 +142,9 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
   };
   load_k(0, 0);
   load_v(0, 0);
-  uint32_t ke = kexp[id], ve = vexp[id];
+  // (behind the last key that of 1: a block to which nobody has stored may have any, and some make a NaN of 0)
+  auto value_scale = [&](int s0) -> uint32_t { return tile_key(s0) < k_end ? vexp[id] : 127u; };
+  uint32_t ke = kexp[id], ve = value_scale(0);
 
   // ---- queries: lane (g, c) holds dimensions 64 i + 16 g + 8 half + (0 .. 7) of row c
   bf16x8 qf[NQ][4];
@@ -194,7 +196,7 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
       load_k(s0, 0);
       load_v(s0, 0);
       ke = kexp[id];
-      ve = vexp[id];
+      ve = value_scale(s0);
     }
     const int here = min(32, steps - s0);
     for (int s = 0; s < here; ++s) {

@@ -127,7 +127,10 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
     const int key0 = k_begin + tile * kTile;
     if (key0 + kTile > min(all_see, k_end)) {  // some row does not see all of it
       asm volatile("");
-      if (key0 + s_key >= k_end) vc = make_uint4(0, 0, 0, 0);
+      if (key0 + s_key >= k_end) {  // (a block to which nobody has stored may have any scale, and some make a NaN of 0)
+        vc = make_uint4(0, 0, 0, 0);
+        ve = 127;
+      }
       if (has_nan(vc.x) || has_nan(vc.y) || has_nan(vc.z) || has_nan(vc.w)) {  // counted below
         atomicMin(&nan_tile, tile);
         vc = make_uint4(vc.x & ~nan_bytes(vc.x), vc.y & ~nan_bytes(vc.y), vc.z & ~nan_bytes(vc.z), vc.w & ~nan_bytes(vc.w));

@@ -194,6 +194,29 @@ def test_sequences_that_share_blocks():
             np.testing.assert_array_equal(t[0, 0, at:at + n].double().cpu().numpy(), pool.rows(0, 0, table[b], 16, n))
 
 
+@pytest.mark.parametrize("byte", [0, 254, 255])
+@pytest.mark.parametrize("dtype,m,group", [("bf16", 1, 4), ("f32", 2, 2), ("bf16", 40, 2)])
+def test_scales_of_blocks_without_rows_do_not_matter(dtype, m, group, byte):
+    """Every block that no sequence holds has a scale byte that no store writes and NaN codes; block 0 is one of them."""
+    rng = np.random.default_rng(650)
+    lens = np.array([[100, 65, 300], [47, 49, 1]])
+    lens = np.maximum(lens, m)
+    k, v, table = build(rng, 2, lens[None], 16)
+    spare = next(p for p in range(k.codes.shape[1]) if p not in table)
+    if spare != 0:                                            # move block 0 there
+        for pool in (k, v):
+            pool.codes[:, spare], pool.byte[:, :, spare] = pool.codes[:, 0], pool.byte[:, :, 0]
+            pool.codes[:, 0] = 0x7F
+        table = np.where(table == 0, spare, table)
+    free = np.array([p for p in range(k.codes.shape[1]) if p not in table])
+    for pool in (k, v):
+        pool.byte[:, :, free] = byte
+    q = queries(rng, 3 * m, 2 * group, dtype)
+    out, lse, status = run(on_device(k, v, table), 0, q, [m] * 3, lens, dtype)
+    assert status == 0
+    check(out, lse, q, [m] * 3, lens, k, v, table, 16, 0, parts_of(dtype, m, group))
+
+
 def test_what_the_binding_refuses(monkeypatch):
     rng = np.random.default_rng(800)
     lens = np.array([[20, 30]])
