@@ -1353,7 +1353,7 @@ int quant_rows(const skipkv_quant_cache *qc, const skipkv_cache *rows, int32_t f
 // Checks an attention call and lays it out; *none: it has no output.
 struct AttendLayout {
   AttendArgs a;
-  size_t o_bytes, total;
+  size_t o_bytes, ml_bytes, total;
   bool none;
 };
 int resolve_attend(const skipkv_quant_cache *qc, const skipkv_queries *qs, AttendLayout *out) {
@@ -1400,9 +1400,10 @@ int resolve_attend(const skipkv_quant_cache *qc, const skipkv_queries *qs, Atten
     const double parts = (double)a.n_entries * a.hw * a.part_rows;
     if (a.n_rb > 65535 || (double)a.n_split * a.n_kv_heads > 2147483647.0 || (a.n_split > 1 && parts > 2147483647.0)) return SKIPKV_ECAPACITY;
     if (a.n_split > 1) {
-      const size_t rows = (size_t)a.n_entries * (size_t)a.n_split * (size_t)a.hw * (size_t)a.part_rows;
+      const size_t rows = (size_t)a.n_parts * (size_t)a.hw * (size_t)a.part_rows;
       l.o_bytes = align_up(rows * SKIPKV_HEAD_DIM * sizeof(float));
-      l.total = l.o_bytes + align_up(rows * sizeof(float2));
+      l.ml_bytes = align_up(rows * sizeof(float2));
+      l.total = l.o_bytes + l.ml_bytes + (a.dealt ? align_up((size_t)(1 + a.n_entries) * 4) : 0);
     }
   }
   *out = l;
@@ -1449,6 +1450,7 @@ int skipkv_quant_attend(const skipkv_quant_cache *qc, int32_t layer, const skipk
   if (l.total > 0) {
     a.part_o = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(ws) + l.o_bytes);
+    if (a.dealt) a.deal = reinterpret_cast<int32_t *>(static_cast<char *>(ws) + l.o_bytes + l.ml_bytes);
   }
   return launch_attend(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SKIPKV_OK : SKIPKV_EHIP;
 }

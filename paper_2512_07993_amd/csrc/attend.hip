@@ -56,6 +56,88 @@ __device__ __forceinline__ void value_frags(const Values &kv, const float (&scal
   }
 }
 
+// The work of a call dealt out by its lengths: all entries' keys in chunks of one length, about the shortest for which there are no more
+// chunks than workgroups, so that no CU is left without work by sequences that are shorter than the longest.  Every wave works this
+// out for itself, with up to kDealt entries (of one block of rows) in each lane, from the same numbers; the first one writes it down
+// for the joining kernel.
+constexpr int kDealt = 4;
+__device__ __forceinline__ int lanes_before_and_here(int v) {  // inclusive prefix sum over the wave
+#define SKIPKV_ROW_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true)
+  SKIPKV_ROW_STEP(0x111, 0xf);  // within rows of 16 lanes: from 1, 2, 4 and 8 lanes before
+  SKIPKV_ROW_STEP(0x112, 0xf);
+  SKIPKV_ROW_STEP(0x114, 0xf);
+  SKIPKV_ROW_STEP(0x118, 0xf);
+  SKIPKV_ROW_STEP(0x142, 0xa);  // the sums of rows 0 and 2 for the rows behind them, then that of the first two
+  SKIPKV_ROW_STEP(0x143, 0xc);
+#undef SKIPKV_ROW_STEP
+  return v;
+}
+template <int HW>
+__device__ __forceinline__ bool deal(const AttendArgs &a, int wg, bool publish, int *b, int *hg, int *split, int *chunk) {
+  constexpr int kUnit = 32 * kWaves / HW;  // keys of a step
+  const int n_hg = a.n_kv_heads / HW, n = (int)a.n_entries, lane = threadIdx.x & 63, per = (n + 63) / 64;
+  const float per_hg = 1.f / (float)n_hg;
+  auto seq_of = [&](int e) { return (int)(((float)e + 0.5f) * per_hg); };  // e / n_hg (both are small)
+  int u[kDealt];  // steps of an entry, one at least; 0: no such entry
+  float all = 0.f;
+#pragma unroll
+  for (int i = 0; i < kDealt; ++i) {
+    const int e = lane * per + i;
+    u[i] = 0;
+    if (i < per && e < n) {
+      const int seq = seq_of(e);
+      int most = 1;
+#pragma unroll
+      for (int x = 0; x < HW; ++x) {
+        const int len = a.len[((e - seq * n_hg) * HW + x) * a.batch + seq];
+        if (length_ok(a, len)) most = max(most, len);
+      }
+      u[i] = (most + kUnit - 1) / kUnit;
+      all += (float)u[i];
+    }
+  }
+  all = row16_sum_fast(all);
+  auto lane_of = [](float v, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); };
+  all = lane_of(all, 0) + lane_of(all, 16) + lane_of(all, 32) + lane_of(all, 48);
+  int c = __builtin_amdgcn_readfirstlane(max(1, (int)(all / (float)a.dealt))), cnt, upto;
+  for (;;) {
+    cnt = 0;
+#pragma unroll
+    for (int i = 0; i < kDealt; ++i)
+      if (i < per) cnt += (u[i] + c - 1) / c;
+    upto = lanes_before_and_here(cnt);
+    if (__builtin_amdgcn_readlane(upto, 63) <= a.dealt) break;
+    c += max(1, c / 32);
+  }
+  *chunk = c * kUnit;
+  if (publish) {
+    int first = upto - cnt;
+    if (lane == 0) a.deal[0] = *chunk;
+#pragma unroll
+    for (int i = 0; i < kDealt; ++i)
+      if (i < per && lane * per + i < n) {
+        a.deal[1 + lane * per + i] = first;
+        first += (u[i] + c - 1) / c;
+      }
+  }
+  const uint64_t behind = __ballot(upto > wg);
+  if (!behind) return false;  // fewer chunks than workgroups
+  const int at = __builtin_ctzll(behind);
+  int first = __builtin_amdgcn_readlane(upto - cnt, at), entry = at * per;
+#pragma unroll
+  for (int i = 0; i < kDealt - 1; ++i)
+    if (i < per - 1) {
+      const int k = (__builtin_amdgcn_readlane(u[i], at) + c - 1) / c;
+      if (wg >= first + k && entry == at * per + i) {
+        ++entry;
+        first += k;
+      }
+    }
+  *split = wg - first;
+  *b = __builtin_amdgcn_readfirstlane(seq_of(entry));
+  *hg = entry - *b * n_hg;
+  return true;
+}
 
 // HW: heads side by side (their rows of a slot are neighbours in memory: 512 bytes at a time come faster than 128), one or more waves to
 // each, which take steps of 32 keys in turn.  DT: type of q and out.
@@ -71,9 +153,18 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
   const int tid = threadIdx.x, wave_all = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave_all / HW, hw = wave_all % HW;
   const int lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int bmask = (1 << a.block_log2) - 1;
-  const int n_hg = a.n_kv_heads / HW, split = blockIdx.x / n_hg, hg = blockIdx.x - split * n_hg, h = hg * HW + hw;
-  const int rb = blockIdx.y, b = blockIdx.z;
-  const int k_begin = split * a.chunk;
+  const int n_hg = a.n_kv_heads / HW;
+  int split, hg, rb = 0, b, chunk = a.chunk;
+  if (a.dealt) {
+    if (!deal<HW>(a, blockIdx.x, blockIdx.x == 0 && wave_all == 0, &b, &hg, &split, &chunk)) return;
+  } else {
+    split = blockIdx.x / n_hg;
+    hg = blockIdx.x - split * n_hg;
+    rb = blockIdx.y;
+    b = blockIdx.z;
+  }
+  const int h = hg * HW + hw;
+  const int k_begin = split * chunk;
   const int32_t *table = a.block_table + (int64_t)b * a.table_stride;
   // Up to 32 steps at a time: lane i looks up the block of tile i & 1 of step i >> 1.  The first look-up waits for nothing: what it
   // finds behind the last key is put right below.
@@ -98,13 +189,13 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
       n_ok = ok;
     }
   }
-  const int n_chunks = max(1, (most + a.chunk - 1) / a.chunk);
+  const int n_chunks = max(1, (most + chunk - 1) / chunk);
   if (!q_ok || r0 >= r1 || split >= n_chunks) {
     if (!q_ok && split == 0 && rb == 0 && lane == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
     return;
   }
   if (!n_ok && split == 0 && lane == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
-  const int k_end = min(n_ok ? rows_see(a, m, n, r1 - 1) : 0, k_begin + a.chunk);
+  const int k_end = min(n_ok ? rows_see(a, m, n, r1 - 1) : 0, k_begin + chunk);
   const int steps_all = max(0, (k_end - k_begin + 31) / 32);
   const int steps = kw < steps_all ? (steps_all - kw + KW - 1) / KW : 0;  // of this wave
   bool poison = !n_ok;
@@ -322,7 +413,8 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
     for (int j4 = 0; j4 < 2; ++j4)
       *reinterpret_cast<float4 *>(&o_part[wave_all][c][32 * g + 8 * i + 4 * j4]) = make_float4(o[4 * j4][i], o[4 * j4 + 1][i], o[4 * j4 + 2][i], o[4 * j4 + 3][i]);
   __syncthreads();
-  const int rows = r1 - r0, entry = (b * a.n_rb + rb) * n_hg + hg;
+  const int rows = r1 - r0;
+  const int64_t part = a.dealt ? (int64_t)blockIdx.x : (int64_t)((b * a.n_rb + rb) * n_hg + hg) * a.n_split + split;
   for (int item = kw * 64 + lane; item < rows * (kD / 4); item += 64 * KW) {
     const int row = item / (kD / 4), d = 4 * (item % (kD / 4)), r = r0 + row;
     float top = kRefInit;
@@ -342,7 +434,7 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
       const int j = r / a.group;
       store_row<DT>(a, q0 + j, h * a.group + r - j * a.group, d, v, top, all);
     } else {
-      const int64_t at = (((int64_t)entry * a.n_split + split) * HW + hw) * a.part_rows + row;
+      const int64_t at = (part * HW + hw) * a.part_rows + row;
       *reinterpret_cast<float4 *>(a.part_o + at * kD + d) = v;
       if (d == 0) a.part_ml[at] = make_float2(top, all);
     }
@@ -362,6 +454,8 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
   const int64_t entry = row_at / per_entry;
   const int in_entry = (int)(row_at - entry * per_entry);
   const bool in = entry < a.n_entries;
+  const int chunk = a.dealt ? a.deal[0] : a.chunk;
+  const int64_t first = !in ? 0 : a.dealt ? a.deal[1 + entry] : entry * a.n_split, bound = a.dealt ? a.n_parts : first + a.n_split;
   constexpr int AHEAD = 8;
   float2 ml[AHEAD];
   float4 x[AHEAD];
@@ -369,8 +463,8 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       const int s = s0 + i * GR + grp;
-      if (in && s < a.n_split) {
-        const int64_t at = (entry * a.n_split + s) * per_entry + in_entry;
+      if (in && first + s < bound) {
+        const int64_t at = (first + s) * per_entry + in_entry;
         ml[i] = a.part_ml[at];
         x[i] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + 4 * d);
       }
@@ -389,7 +483,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
       const int n = a.len[(hg * a.hw + i) * a.batch + b];
       if (length_ok(a, n)) most = max(most, rows_see(a, m, n, r1 - 1));
     }
-    if (q_ok && r < r1) n_chunks = (most + a.chunk - 1) / a.chunk;
+    if (q_ok && r < r1) n_chunks = (most + chunk - 1) / chunk;
   }
   if (n_chunks <= 1) n_chunks = 0;  // written already
   if (GR == 8 && n_chunks == 0) return;
@@ -460,9 +554,11 @@ void plan_attend(AttendArgs *a) {
     const int64_t want = std::max<int64_t>(1, 256 / a->n_entries);
     a->chunk = (int32_t)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
     a->n_split = std::max(1, (a->max_len + a->chunk - 1) / a->chunk);
+    a->n_parts = a->n_entries * a->n_split;
     return;
   }
   double best = 0;
+  int steps = 0;  // of a workgroup
   for (const int hw : {4, 2, 1}) {
     if (a->n_kv_heads % hw) continue;
     const int unit = 32 * kWaves / hw, units = std::max(1, (a->max_len + unit - 1) / unit);
@@ -479,13 +575,21 @@ void plan_attend(AttendArgs *a) {
         a->chunk = per * unit;
         a->n_split = split;
         a->n_entries = entries;
+        steps = per;
       }
     }
   }
+  a->n_parts = a->n_entries * a->n_split;
+  // Dealing costs a workgroup 2 us before its first key and pays where lengths differ, us, as planned for equal lengths / dealt:
+  //   steps  8: 16 x 8 heads, 512-4096 keys 22.6 / 23.4;  8 x 8 heads, 1-8 K 22.0 / 22.4
+  //   steps 16: 16 x 8 heads, 1-8 K 39.5 / 36.1;  8 x 8 heads, 2-16 K 39.3 / 37.0;  all 4000-4500 35.3 / 36.4
+  //   steps 32 and more: 16 x 8 heads, 2-16 K 65.2 / 58.4;  60 x 4 heads, 2-16 K 122 / 105;  all 32896 103.9 / 106.2
+  if (a->n_split > 1 && steps >= 12 && a->batch > 1 && a->n_rb == 1 && a->n_entries <= 64 * kDealt)
+    a->dealt = (int32_t)(a->n_parts = (a->n_parts + 255) / 256 * 256);
 }
 
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
-  const dim3 grid(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
+  const dim3 grid = a.dealt ? dim3((unsigned)a.dealt) : dim3(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
   auto go = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     if (a.rows > 16) (void)launch_attend_rows(a, st);

@@ -372,9 +372,11 @@ struct AttendArgs {
   int32_t hw;                     // heads side by side in a workgroup
   int32_t chunk, n_split;         // keys per workgroup; chunks of an entry (sequence, block of rows, group of heads), at most
   int32_t part_rows;              // rows per chunk's partial results
-  int64_t n_entries;
-  float *part_o;                  // [n_entries, n_split, hw, part_rows, 128] outputs before the division
-  float2 *part_ml;                // [n_entries, n_split, hw, part_rows] (reference, sum), log2 domain
+  int32_t dealt;                  // workgroups that are dealt out by the lengths (0: chunk and n_split as they stand)
+  int64_t n_entries, n_parts;     // chunks of all entries, at most
+  float *part_o;                  // [n_parts, hw, part_rows, 128] outputs before the division
+  float2 *part_ml;                // [n_parts, hw, part_rows] (reference, sum), log2 domain
+  int32_t *deal;                  // [1 + n_entries] keys per workgroup; an entry's first chunk
   int32_t *dev_status;
 };
 void plan_attend(AttendArgs *a);

@@ -30,6 +30,85 @@ def test_heads_of_different_length_in_cut_caches(heads, dtype, m, group):
     check(out, lse, q, [m, m], lens, k, v, table, 16, 0, parts_of(dtype, m, group))
 
 
+DEALT = {
+    "one long, others short": lambda rng, hk, n: np.where(np.arange(n)[None, :] == n // 2, 20000, rng.integers(1, 60, (hk, n))),
+    "spread": lambda rng, hk, n: rng.integers(1, 20001, (hk, n)),
+    "nothing anywhere": lambda rng, hk, n: np.zeros((hk, n), dtype=np.int64),
+    "all the same": lambda rng, hk, n: np.full((hk, n), 6000),
+    "one key each": lambda rng, hk, n: np.ones((hk, n), dtype=np.int64),
+    "heads apart": lambda rng, hk, n: np.where(np.arange(hk)[:, None] == hk - 1, 20000, rng.integers(0, 5, (hk, n))),
+}
+
+
+@pytest.mark.parametrize("heads,batch", [(4, 12), (3, 20), (2, 65), (1, 130), (8, 33)])
+@pytest.mark.parametrize("how", list(DEALT))
+def test_chunks_dealt_out_by_the_lengths(how, heads, batch):
+    """max_len is far above most lengths: the chunks follow the lengths.  One pool of few blocks serves all sequences."""
+    rng = np.random.default_rng(900 + batch)
+    lens = np.minimum(DEALT[how](rng, heads, batch), 20000)
+    table = np.tile(rng.integers(0, 40, 20000 // 128 + 1).astype(np.int32), (batch, 1))
+    for b in range(batch):
+        table[b] = np.roll(table[b], b)
+    pools = [Pool(1, 40, 128, heads) for _ in range(2)]
+    for pool in pools:
+        pool.codes[:] = rng.integers(0, 127, pool.codes.shape) + 128 * rng.integers(0, 2, pool.codes.shape)
+        pool.byte[:] = rng.integers(112, 119, pool.byte.shape)
+    q = queries(rng, batch, heads * 2, "bf16")
+    out, lse, status = run(on_device(*pools, table), 0, q, [1] * batch, lens, "bf16", max_len=20000)
+    assert status == 0
+    some = sorted(set(rng.integers(0, batch, 6)) | {0, batch // 2, batch - 1})
+    at = torch.tensor(some, device="cuda")
+    check(out[at], lse[at], q[at], [1] * len(some), lens[:, some], *pools, table[some], 128, 0, parts_of("bf16", 1, 2))
+    again, _, _ = run(on_device(*pools, table), 0, q, [1] * batch, lens, "bf16", max_len=20000)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_dealt_chunks_with_lengths_blocks_and_offsets_that_do_not_fit(dtype):
+    rng = np.random.default_rng(950)
+    lens = np.array([[9000, 20, 16000, 300, 7000, 50]]).repeat(4, 0)
+    lens[1] = lens[1][::-1]
+    k, v, table = build(rng, 4, lens[None], 128, width=400)
+    ms, longest = [1, 2, 0, 1, 3, 1], 400 * 128
+    q = queries(rng, sum(ms), 4, dtype)
+    clean, clse, status = run(on_device(k, v, table), 0, q, ms, lens, dtype, max_len=longest)
+    assert status == 0
+    check(clean, clse, q, ms, lens, k, v, table, 128, 0, parts_of(dtype, 3, 1))
+    bad, t2 = lens.copy(), table.copy()
+    bad[0, 0], bad[2, 4] = longest + 1, -1
+    t2[3, 1] = k.codes.shape[1]
+    out, lse, status = run(on_device(k, v, t2), 0, q, ms, bad, dtype, max_len=longest)
+    assert status == B.DEV_BAD_LENGTHS | B.DEV_BAD_BLOCK_TABLE
+    row = {0: [0], 1: [1, 2], 3: [3], 4: [4, 5, 6], 5: [7]}
+    gone = torch.zeros(sum(ms), 4, dtype=torch.bool, device="cuda")
+    gone[row[0], 0] = True
+    gone[row[4], 2] = True
+    for h in range(4):                                       # the second block of sequence 3: heads that reach it
+        gone[row[3], h] = bool(lens[h, 3] > 128)
+    assert bool(torch.isnan(out[gone]).all()) and bool(torch.isfinite(out[~gone]).all())
+    for h in range(4):
+        bs_ = [b for b in (0, 1, 4, 5) if not ((b == 0 and h == 0) or (b == 4 and h == 2))]
+        rows_ = [i for b in bs_ for i in row[b]]
+        check(out[rows_][:, h:h + 1], lse[rows_][:, h:h + 1], q[rows_][:, h:h + 1], [ms[b] for b in bs_], lens[h:h + 1, bs_],
+              _head(k, h), _head(v, h), table[bs_], 128, 0, parts_of(dtype, 3, 1))
+    # offsets that descend: that sequence has no output, the others theirs
+    off = np.concatenate([[0], np.cumsum(ms)]).astype(np.int32)
+    off[2] = 0
+    res = torch.full_like(q, 99.0)
+    qs = B.Queries(q, res, _cuda(off), max_q=3, max_len=longest, scale=SCALE)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    qc = on_device(k, v, table)
+    ws = torch.empty(B.skipkv_quant_attend_workspace_bytes(qc, qs) + 256, dtype=torch.uint8, device="cuda").fill_(0xFF)
+    B.skipkv_quant_attend(qc, 0, qs, _cuda(lens.astype(np.int32)), ws, status)
+    assert int(status.item()) == B.DEV_BAD_LENGTHS and bool((res[[4, 5, 6, 7]] != 99.0).all())
+
+
+def _head(pool, h):
+    one = Pool(1, pool.codes.shape[1], pool.codes.shape[2], 1)
+    one.codes, one.byte = pool.codes[:, :, :, h:h + 1], pool.byte[:, h:h + 1]
+    return one
+
+
 @pytest.mark.parametrize("layout", ["slots", "heads"])
 @pytest.mark.parametrize("batch,heads", [(1, 4), (40, 4), (3, 2)])
 def test_one_and_many_sequences_in_both_layouts(layout, batch, heads):
