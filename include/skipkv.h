@@ -640,7 +640,8 @@ typedef struct skipkv_queries {
  * additions the result does not depend on max_len and max_q.  A length that is negative, above
  * max_len or above table_stride * block_size (SKIPKV_DEV_BAD_LENGTHS), or a block id outside [0, n_blocks) among a head's
  * blocks (SKIPKV_DEV_BAD_BLOCK_TABLE), makes the rows concerned NaN; a sequence whose q_off entries
- * descend, leave [0, total_q] or are more than max_q apart gets no output (SKIPKV_DEV_BAD_LENGTHS).
+ * descend, leave [0, total_q] or are more than max_q apart gets no output (SKIPKV_DEV_BAD_LENGTHS), nor, where entries
+ * that descend make the sequences longer than total_q in all, may the last ones.
  * dev_status  device int32, OR-ed into; may be NULL.
  * ws    device scratch of at least skipkv_quant_attend_workspace_bytes (0 is possible: then ws may be
  *       NULL), 256-byte aligned.

@@ -60,18 +60,6 @@ __device__ __forceinline__ void value_frags(const Values &kv, const float (&scal
 // chunks than workgroups, so that no CU is left without work by sequences that are shorter than the longest.  Every wave works this
 // out for itself, with up to kDealt entries (of one block of rows) in each lane, from the same numbers; the first one writes it down
 // for the joining kernel.
-constexpr int kDealt = 4;
-__device__ __forceinline__ int lanes_before_and_here(int v) {  // inclusive prefix sum over the wave
-#define SKIPKV_ROW_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true)
-  SKIPKV_ROW_STEP(0x111, 0xf);  // within rows of 16 lanes: from 1, 2, 4 and 8 lanes before
-  SKIPKV_ROW_STEP(0x112, 0xf);
-  SKIPKV_ROW_STEP(0x114, 0xf);
-  SKIPKV_ROW_STEP(0x118, 0xf);
-  SKIPKV_ROW_STEP(0x142, 0xa);  // the sums of rows 0 and 2 for the rows behind them, then that of the first two
-  SKIPKV_ROW_STEP(0x143, 0xc);
-#undef SKIPKV_ROW_STEP
-  return v;
-}
 template <int HW>
 __device__ __forceinline__ bool deal(const AttendArgs &a, int wg, bool publish, int *b, int *hg, int *split, int *chunk) {
   constexpr int kUnit = 32 * kWaves / HW;  // keys of a step
@@ -551,6 +539,17 @@ void plan_attend(AttendArgs *a) {
   if (a->rows > 16) {  // one workgroup per CU
     a->hw = 1;
     a->n_entries = (int64_t)a->batch * a->n_rb * a->n_kv_heads;
+    // Up to 128 blocks of rows are cut alike here; more are dealt out by what the sequences have, us, as cut here / dealt: 8 x 8 heads, 100-400
+    // query tokens over 2-6 K keys 215 / 180;  4 x 8 heads, 700-1500 tokens 295 / 282;  30 x 8 heads, 20-40 tokens 133 / 136;  and
+    // 32 blocks in all 23.2 / 26.4.
+    const int64_t blocks = std::min<int64_t>((int64_t)a->batch * a->n_rb, ((int64_t)a->total_q * a->group + a->rows - 1) / a->rows + a->batch) * a->n_kv_heads;
+    if (a->n_entries > 128 && a->batch <= 64 * kDealt && blocks < (1 << 22)) {  // (a grid has fewer than 2^32 threads)
+      a->chunk = a->max_len;
+      a->n_split = 1;
+      a->n_parts = kRowParts;
+      a->dealt = (int32_t)blocks + kRowParts;
+      return;
+    }
     const int64_t want = std::max<int64_t>(1, 256 / a->n_entries);
     a->chunk = (int32_t)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
     a->n_split = std::max(1, (a->max_len + a->chunk - 1) / a->chunk);
@@ -596,7 +595,7 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
     else if (a.hw == 4) hipLaunchKernelGGL((k_attend<DT, 4>), grid, dim3(64 * kWaves), 0, st, a);
     else if (a.hw == 2) hipLaunchKernelGGL((k_attend<DT, 2>), grid, dim3(64 * kWaves), 0, st, a);
     else hipLaunchKernelGGL((k_attend<DT, 1>), grid, dim3(64 * kWaves), 0, st, a);
-    if (a.n_split == 1) return;
+    if (a.n_split == 1) return;  // (or joined already)
     const int64_t rows = a.n_entries * a.hw * a.part_rows;
     if (a.n_split > 8) hipLaunchKernelGGL((k_attend_join<DT, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_attend_join<DT, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a);

@@ -24,6 +24,17 @@ __device__ __forceinline__ bool length_ok(const AttendArgs &a, int n) {
   return n >= 0 && n <= a.max_len && n <= (a.table_stride << a.block_log2);
 }
 
+__device__ __forceinline__ int lanes_before_and_here(int v) {  // inclusive prefix sum over the wave
+#define SKIPKV_ROW_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true)
+  SKIPKV_ROW_STEP(0x111, 0xf);  // within rows of 16 lanes: from 1, 2, 4 and 8 lanes before
+  SKIPKV_ROW_STEP(0x112, 0xf);
+  SKIPKV_ROW_STEP(0x114, 0xf);
+  SKIPKV_ROW_STEP(0x118, 0xf);
+  SKIPKV_ROW_STEP(0x142, 0xa);  // the sums of rows 0 and 2 for the rows behind them, then that of the first two
+  SKIPKV_ROW_STEP(0x143, 0xc);
+#undef SKIPKV_ROW_STEP
+  return v;
+}
 // x as a sum of N bf16 numbers, the rest of each in the next; pairs of x, y packed.
 template <int N>
 __device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&out)[N]) {

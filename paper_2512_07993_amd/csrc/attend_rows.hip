@@ -46,13 +46,101 @@ __device__ __forceinline__ uint4 load_codes(const uint8_t *p) {
   return make_uint4(x.x, x.y, y.x, y.y);
 }
 
+// Keys of a piece: whole tiles.
+__device__ __forceinline__ int piece_keys(int keys, int pieces) { return max(1, ((keys + kTile - 1) / kTile + pieces - 1) / pieces) * kTile; }
+
+// Blocks of 256 rows dealt out: as many as make whole turns of the 256 CUs run over all their keys; the others, which would leave CUs
+// without work at the end, are cut into `pieces` along the keys, as many as come out shortest.  (600 blocks of 53 tiles: three turns take
+// 161 tiles' time, 88 blocks in two pieces 139, an even share of all would be 125.)
+struct RowDeal {
+  int blocks, whole, pieces;  // blocks of all sequences and heads; those that are not cut
+};
+__device__ __forceinline__ bool deal_rows(const AttendArgs &a, int wg, bool publish, int *b, int *rb, int *h, RowDeal *deal, int *piece) {
+  const int lane = threadIdx.x & 63, per = (a.batch + 63) / 64;
+  int cnt = 0, u[kDealt];
+  float keys = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < kDealt; ++i) {
+    const int seq = lane * per + i;
+    u[i] = 0;
+    if (i < per && seq < a.batch) {
+      int q0, m;
+      const int len = a.len[seq];
+      if (!seq_queries(a, seq, &q0, &m)) bad = true;
+      else u[i] = (m * a.group + a.rows - 1) / a.rows;
+      if (length_ok(a, len)) keys += (float)u[i] * (float)len;
+      cnt += u[i];
+    }
+  }
+  const int upto = lanes_before_and_here(cnt), n = __builtin_amdgcn_readlane(upto, 63);
+  keys = row16_sum_fast(keys);
+  auto lane_of = [](float v, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); };
+  keys = lane_of(keys, 0) + lane_of(keys, 16) + lane_of(keys, 32) + lane_of(keys, 48);
+  const int blocks = n * a.n_kv_heads, whole = blocks / 256 * 256, rest = blocks - whole;
+  // us: a tile of 64 keys 1.9 and three of them before the first one; a piece's partial results 0.05, their joining 5
+  int pieces = 1;
+  if (rest > 0) {
+    const float tiles = keys / (64.f * (float)max(n, 1));  // of a block, about
+    float best = 0.f;
+    for (int p = 1; p <= 8 && p * rest <= kRowParts && (p == 1 || tiles >= 4.f * (float)p); ++p) {
+      const float us = (float)((rest * p + 255) / 256) * (tiles / (float)p + 3.f) * 1.9f + (p > 1 ? 5.f + 0.05f * (float)(rest * p) : 0.f);
+      if (p == 1 || us < best) {
+        best = us;
+        pieces = p;
+      }
+    }
+  }
+  pieces = __builtin_amdgcn_readfirstlane(pieces);
+  *deal = RowDeal{blocks, whole, pieces};
+  if (publish) {
+    int first = upto - cnt;
+    if (lane == 0) a.deal[0] = whole, a.deal[1] = pieces;
+#pragma unroll
+    for (int i = 0; i < kDealt; ++i)
+      if (i < per && lane * per + i < a.batch) a.deal[2 + lane * per + i] = (first += u[i]);
+    if (bad && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
+  }
+  const int block = wg < whole ? wg : whole + (wg - whole) / pieces;
+  *piece = wg < whole ? 0 : (wg - whole) % pieces;
+  if (block >= blocks) return false;
+  const int at_block = block / a.n_kv_heads;
+  *h = block - at_block * a.n_kv_heads;
+  const int at = __builtin_ctzll(__ballot(upto > at_block));
+  int first = __builtin_amdgcn_readlane(upto - cnt, at), seq = at * per;
+#pragma unroll
+  for (int i = 0; i < kDealt - 1; ++i) {
+    const int k = __builtin_amdgcn_readlane(u[i], at);
+    if (i < per - 1 && at_block >= first + k && seq == at * per + i) {
+      ++seq;
+      first += k;
+    }
+  }
+  const int of_seq = __builtin_amdgcn_readlane(u[0], at);
+  int mine = of_seq;  // blocks of the sequence
+#pragma unroll
+  for (int i = 1; i < kDealt; ++i)
+    if (seq == at * per + i) mine = __builtin_amdgcn_readlane(u[i], at);
+  *b = seq;
+  *rb = mine - 1 - (at_block - first);  // the rows that see most first
+  return true;
+}
+
 __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a) {
   __shared__ __align__(256) char tiles[3][kTileB];
   __shared__ int nan_tile;                              // first tile with a NaN in V that only some rows see
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
   const int bmask = (1 << a.block_log2) - 1;
-  const int split = blockIdx.x / a.n_kv_heads, h = blockIdx.x - split * a.n_kv_heads;
-  const int rb = a.n_rb - 1 - blockIdx.y, b = blockIdx.z;  // (the rows that see most first)
+  int split, h, rb, b;
+  RowDeal dealt{0, 0, 1};
+  if (a.dealt) {
+    if (!deal_rows(a, blockIdx.x, blockIdx.x == 0 && wave == 0, &b, &rb, &h, &dealt, &split)) return;
+  } else {
+    split = blockIdx.x / a.n_kv_heads;
+    h = blockIdx.x - split * a.n_kv_heads;
+    rb = a.n_rb - 1 - blockIdx.y;  // (the rows that see most first)
+    b = blockIdx.z;
+  }
   int q0, m;
   const bool q_ok = seq_queries(a, b, &q0, &m);
   const int n = a.len[h * a.batch + b];
@@ -64,9 +152,10 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
   const bool n_ok = length_ok(a, n);
   if (!n_ok && split == 0 && tid == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_LENGTHS);
   const int most = n_ok ? rows_see(a, m, n, r1 - 1) : 0;
-  const int n_chunks = max(1, (most + a.chunk - 1) / a.chunk);
+  const int chunk = !a.dealt ? a.chunk : (int)blockIdx.x < dealt.whole ? max(most, 1) : piece_keys(most, dealt.pieces);
+  const int n_chunks = max(1, (most + chunk - 1) / chunk);
   if (split >= n_chunks) return;
-  const int k_begin = split * a.chunk, k_end = min(most, k_begin + a.chunk);
+  const int k_begin = split * chunk, k_end = min(most, k_begin + chunk);
   const int n_tiles = (k_end - k_begin + kTile - 1) / kTile;
   const int all_see = max(0, n - m + r0 / a.group + 1);  // keys below this are seen by every row of the workgroup
   if (tid == 0) nan_tile = 0x7FFFFFFF;
@@ -327,7 +416,8 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
   const float all = poison ? nan32() : sum + __shfl_xor(sum, 32);
   if (r >= r1) return;
   const int j = r / a.group, head = h * a.group + r - j * a.group;
-  const int64_t at = (((int64_t)(b * a.n_rb + rb) * a.n_kv_heads + h) * a.n_split + split) * a.part_rows + (r - r0);
+  const int64_t place = a.dealt ? (int64_t)((int)blockIdx.x - dealt.whole) : ((int64_t)(b * a.n_rb + rb) * a.n_kv_heads + h) * a.n_split + split;
+  const int64_t at = place * a.part_rows + (r - r0);
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -343,11 +433,56 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
     }
 }
 
+// Joins the pieces of the blocks that were cut: 32 lanes per row, four dimensions each.
+__global__ void __launch_bounds__(256) k_attend_join_rows(AttendArgs a) {
+  const int whole = a.deal[0], pieces = a.deal[1], rest = a.deal[1 + a.batch] * a.n_kv_heads - whole, d = threadIdx.x & 31;
+  if (pieces <= 1) return;
+  for (int item = blockIdx.x * 8 + (threadIdx.x >> 5); item < rest * a.part_rows; item += gridDim.x * 8) {
+    const int cut = item / a.part_rows, row = item - cut * a.part_rows, at_block = (whole + cut) / a.n_kv_heads, h = whole + cut - at_block * a.n_kv_heads;
+    float2 ml[8];
+    float4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)  // (under way before it is known how many there are)
+      if (i < pieces) {
+        const int64_t at = (int64_t)(cut * pieces + i) * a.part_rows + row;
+        ml[i] = a.part_ml[at];
+        x[i] = *reinterpret_cast<const float4 *>(a.part_o + at * kD + 4 * d);
+      }
+    int lo = 0, hi = a.batch - 1;  // the first sequence whose blocks end behind this one
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (a.deal[2 + mid] > at_block) hi = mid;
+      else lo = mid + 1;
+    }
+    int q0, m;
+    (void)seq_queries(a, lo, &q0, &m);
+    const int rb = a.deal[2 + lo] - 1 - at_block, r0 = rb * a.rows, r1 = min(r0 + a.rows, m * a.group), r = r0 + row, n = a.len[h * a.batch + lo];
+    if (r >= r1) continue;
+    const int most = length_ok(a, n) ? rows_see(a, m, n, r1 - 1) : 0, chunk = piece_keys(most, pieces), n_chunks = (most + chunk - 1) / chunk;
+    if (n_chunks <= 1) continue;  // written already
+    float top = kRefInit, all = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n_chunks) top = fmaxf(top, ml[i].x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n_chunks) {
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+        all += ml[i].y * f;
+        v.x += x[i].x * f, v.y += x[i].y * f, v.z += x[i].z * f, v.w += x[i].w * f;
+      }
+    const int j = r / a.group;
+    store_row<SKIPKV_BF16>(a, q0 + j, h * a.group + r - j * a.group, 4 * d, v, top, all);
+  }
+}
+
 }  // namespace
 
 hipError_t launch_attend_rows(const AttendArgs &a, hipStream_t st) {
-  const dim3 grid(a.n_split * a.n_kv_heads, a.n_rb, a.batch);
+  const dim3 grid = a.dealt ? dim3((unsigned)a.dealt) : dim3(a.n_split * a.n_kv_heads, a.n_rb, a.batch);
   hipLaunchKernelGGL(k_attend_rows, grid, dim3(64 * kRowWaves), 0, st, a);
+  if (a.dealt) hipLaunchKernelGGL(k_attend_join_rows, dim3(1024), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -376,9 +376,11 @@ struct AttendArgs {
   int64_t n_entries, n_parts;     // chunks of all entries, at most
   float *part_o;                  // [n_parts, hw, part_rows, 128] outputs before the division
   float2 *part_ml;                // [n_parts, hw, part_rows] (reference, sum), log2 domain
-  int32_t *deal;                  // [1 + n_entries] keys per workgroup; an entry's first chunk
+  int32_t *deal;                  // [1 + n_entries] keys per workgroup; an entry's first chunk; or [2 + batch], see k_attend_rows
   int32_t *dev_status;
 };
+constexpr int kDealt = 4;         // entries (sequences) per lane where the work is dealt out by the lengths
+constexpr int kRowParts = 512;    // partial results of blocks of 256 rows
 void plan_attend(AttendArgs *a);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st);
 hipError_t launch_attend_rows(const AttendArgs &a, hipStream_t st);

@@ -147,6 +147,50 @@ def test_many_rows_over_a_long_cache():
     assert bool((out[:40, 8:] == 0).all()) and bool((lse[:40, 8:] == -np.inf).all())
 
 
+@pytest.mark.parametrize("ms,longest,width", [
+    ([300, 1, 0, 500, 64], 1500, 12), ([0, 0, 700, 0, 0], 2600, 30), ([257] * 9, 900, 8), ([3] * 70 + [260], 300, 4), ([130, 260, 390], 40, 4)])
+def test_many_rows_dealt_out(ms, longest, width):
+    """More blocks of rows than half the CUs: whole turns first, the rest cut along the keys; sequences with few rows or none between."""
+    rng = np.random.default_rng(410 + len(ms))
+    heads, batch = 8, len(ms)
+    lens = np.maximum(rng.integers(1, longest + 1, (heads, batch)), np.array(ms)[None, :] - 5)
+    lens[2, 0], lens[3, batch - 1] = 0, max(longest, ms[-1])
+    table = rng.integers(0, 40, (batch, width)).astype(np.int32)
+    lens = np.minimum(lens, width * 128)
+    pools = [Pool(1, 40, 128, heads) for _ in range(2)]
+    for pool in pools:
+        pool.codes[:] = rng.integers(0, 127, pool.codes.shape) + 128 * rng.integers(0, 2, pool.codes.shape)
+        pool.byte[:] = rng.integers(112, 119, pool.byte.shape)
+    q = queries(rng, sum(ms), heads * 4, "bf16")
+    out, lse, status = run(on_device(*pools, table), 0, q, ms, lens, "bf16")
+    assert status == 0
+    check(out, lse, q, ms, lens, *pools, table, 128, 0, parts_of("bf16", max(ms), 4), heads=[0, 2, 3, 7])
+    again, _, _ = run(on_device(*pools, table), 0, q, ms, lens, "bf16")
+    assert torch.equal(out, again)
+    # one head's length and one sequence's block that do not fit
+    bad, t2 = lens.copy(), table.copy()
+    bad[1, 0] = -1
+    t2[batch - 1, 0] = 40
+    got, gl, status = run(on_device(*pools, t2), 0, q, ms, bad, "bf16", max_len=int(lens.max()))
+    gone = torch.zeros(out.shape[:2], dtype=torch.bool, device="cuda")
+    gone[:ms[0], 4:8] = True
+    for h in range(heads):
+        if ms[-1] and lens[h, batch - 1] > 0:
+            gone[sum(ms) - ms[-1]:, 4 * h:4 * h + 4] = True
+    assert (status & B.DEV_BAD_LENGTHS != 0) == (ms[0] > 0) and (status & B.DEV_BAD_BLOCK_TABLE != 0) == (ms[-1] > 0)
+    assert bool(torch.isnan(got[gone]).all()) and bool(torch.isfinite(got[~gone]).all())
+    off = np.concatenate([[0], np.cumsum(ms)]).astype(np.int32)
+    off[0] = -1
+    qs = B.Queries(q, torch.zeros_like(q), _cuda(off), max_q=max(ms), max_len=int(lens.max()), scale=SCALE)
+    qc, st = on_device(*pools, table), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.skipkv_quant_attend_workspace_bytes(qc, qs) + 256, dtype=torch.uint8, device="cuda").fill_(0xFF)
+    B.skipkv_quant_attend(qc, 0, qs, _cuda(lens.astype(np.int32)), ws, st)
+    live = torch.isfinite(out)                                # (an output may be NaN or not; here none is)
+    assert int(st.item()) == B.DEV_BAD_LENGTHS and bool(live.all()) and bool((qs.out[:ms[0]] == 0).all())
+    if sum(ms) > ms[0]:
+        check(qs.out[ms[0]:], None, q[ms[0]:], ms[1:], lens[:, 1:], *pools, table[1:], 128, 0, parts_of("bf16", max(ms), 4), heads=[5])
+
+
 def test_many_rows_with_lengths_and_blocks_that_do_not_fit():
     rng = np.random.default_rng(401)
     lens = np.array([[700, 300, 520], [80, 310, 90]])
