@@ -582,7 +582,7 @@ void plan_attend(AttendArgs *a) {
   // Dealing costs a workgroup 2 us before its first key and pays where lengths differ, us, as planned for equal lengths / dealt:
   //   steps  8: 16 x 8 heads, 512-4096 keys 22.6 / 23.4;  8 x 8 heads, 1-8 K 22.0 / 22.4
   //   steps 16: 16 x 8 heads, 1-8 K 39.5 / 36.1;  8 x 8 heads, 2-16 K 39.3 / 37.0;  all 4000-4500 35.3 / 36.4
-  //   steps 32 and more: 16 x 8 heads, 2-16 K 65.2 / 58.4;  60 x 4 heads, 2-16 K 122 / 105;  all 32896 103.9 / 106.2
+  //   steps 32 and more: 16 x 8 heads, 2-16 K 65.2 / 57.0;  60 x 4 heads, 2-16 K 122 / 105;  all 32896 103.9 / 106.2
   if (a->n_split > 1 && steps >= 12 && a->batch > 1 && a->n_rb == 1 && a->n_entries <= 64 * kDealt)
     a->dealt = (int32_t)(a->n_parts = (a->n_parts + 255) / 256 * 256);
 }
@@ -597,7 +597,9 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
     else hipLaunchKernelGGL((k_attend<DT, 1>), grid, dim3(64 * kWaves), 0, st, a);
     if (a.n_split == 1) return;  // (or joined already)
     const int64_t rows = a.n_entries * a.hw * a.part_rows;
-    if (a.n_split > 8) hipLaunchKernelGGL((k_attend_join<DT, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    // eight chunks of a row at a time from nine on; dealt out, a row may have more than the mean: from eight on (16 x 8 heads, 2-16 K keys: 57.0
+    // us instead of 59.0; four on average, 32 x 8 heads, 1-8 K: 66.4 instead of 64.4)
+    if (a.dealt ? a.n_parts >= 8 * a.n_entries : a.n_split > 8) hipLaunchKernelGGL((k_attend_join<DT, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_attend_join<DT, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a);
   };
   if (a.dtype == SKIPKV_F32) go(std::integral_constant<int, SKIPKV_F32>{});

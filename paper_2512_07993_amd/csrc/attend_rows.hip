@@ -7,13 +7,14 @@
 // weights from there as they lie: the keys of a matrix instruction are 16 k + 4 hi + (0 .. 3) and 8 further on, which transposing
 // reads of V's rows deliver in that order.
 //
-// What bounds it: the matrix pipe is busy for 44 % of the time and vector instructions are issued for 48 %; a SIMD overlaps the two up to
-// some six vector instructions per matrix instruction of 32 cycles (18.8 ns against 15.5 alone, 23 with eight), and this has 6.4: per weight
+// What bounds it: the matrix pipe is busy for 47 % of the time and vector instructions are issued for 51 %; a SIMD overlaps the two up to
+// some six vector instructions per matrix instruction of 32 cycles (18.8 ns against 15.5 alone, 23 with eight), and this has 6.5: per weight
 // an fma, an exponential (two issue slots), an addition, half a conversion and half a maximum, besides the staging.  So everything but the
 // matrix instructions is dealt out evenly among them; operands are in registers a block of 32 keys ahead; rows in shared memory are
 // padded, not swizzled, so that addresses are immediates.  4 sequences of 3.5-4.3 K keys, 1.0-1.5 K query tokens, 8 x 4 heads (256 GFLOP):
-// 300 us, 854 TFLOP/s (a library's product of 8192 x 8192 matrices reaches 1.2-1.3 PFLOP/s); with all weights before the product, with
-// swizzled addresses 322 us, without the pipeline across blocks 345 us.  32 x 32 tiles with 64 rows per wave need more registers than two waves on a
+// 283 to 304 us from run to run, 840-900 TFLOP/s (a library's product of square matrices reaches 1.2-1.3 PFLOP/s); before blocks were dealt
+// out 294 to 316: 11 us less each time; before that, with all weights before the product and swizzled addresses 7 % more, without
+// the pipeline across blocks 15 % more.  32 x 32 tiles with 64 rows per wave need more registers than two waves on a
 // SIMD have (544 us).
 #include <algorithm>
 #include <type_traits>
