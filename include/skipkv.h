@@ -636,7 +636,7 @@ typedef struct skipkv_queries {
  * a query does not see have no influence on it, whatever they hold.
  * len   device [n_kv_heads, batch]: this layer's lengths, the query tokens included.
  * fp32 queries enter as three bf16 parts and fp32 weights of the softmax as three, those of bf16 queries as two, or as one where a
- * KV head has more than 16 (from 2048 slots on 32) rows max_q * n_q_heads / n_kv_heads.  But for that and the order of
+ * KV head has more than 32 rows (max_q * n_q_heads / n_kv_heads) and these are taken 256 at a time.  But for that and the order of
  * additions the result does not depend on max_len and max_q.  A length that is negative, above
  * max_len or above table_stride * block_size (SKIPKV_DEV_BAD_LENGTHS), or a block id outside [0, n_blocks) among a head's
  * blocks (SKIPKV_DEV_BAD_BLOCK_TABLE), makes the rows concerned NaN; a sequence whose q_off entries

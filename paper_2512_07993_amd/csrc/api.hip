@@ -1403,7 +1403,7 @@ int resolve_attend(const skipkv_quant_cache *qc, const skipkv_queries *qs, Atten
       const size_t rows = (size_t)a.n_parts * (size_t)a.hw * (size_t)a.part_rows;
       l.o_bytes = align_up(rows * SKIPKV_HEAD_DIM * sizeof(float));
       l.ml_bytes = align_up(rows * sizeof(float2));
-      l.total = l.o_bytes + l.ml_bytes + (a.dealt ? align_up((size_t)(2 + (a.rows > 16 ? a.batch : a.n_entries)) * 4) : 0);
+      l.total = l.o_bytes + l.ml_bytes + (a.dealt ? align_up((size_t)(2 + (a.rows == 256 ? a.batch : a.n_entries)) * 4) : 0);
     }
   }
   *out = l;

@@ -1,6 +1,6 @@
 // Attention over the 8-bit cache: for every query row r of a (sequence, KV head), out = sum_t p_t v_t with
 // p = softmax(scale * q.k_t) over the keys that the row sees, in one pass over K and V with a running reference and sum.
-// This file: up to 16 rows at a time (decode, drafted tokens), where the cache's bytes are what counts.
+// This file: 16 or 32 rows at a time (decode, drafted tokens), where the cache's bytes are what counts.
 //
 // Everything is computed transposed, so that nothing has to change lanes between the two products: S^T = K Q^T leaves lane (g, c)
 // of a 16 x 16 tile (g = lane / 16, c = lane % 16) with the logits of query row c for keys 4g .. 4g+3, and O^T = V^T P^T wants from that
@@ -22,7 +22,7 @@ namespace skipkv {
 namespace {
 
 constexpr int kOPitch = kD + 4;  // floats per row of the merge buffer: 16 rows start at different banks
-constexpr int kWaves = 8;        // per workgroup; two workgroups share a CU (one with fp32 queries)
+constexpr int kWaves = 8;        // per workgroup; two workgroups share a CU (one with fp32 queries or 32 rows)
 // 32 keys of a wave: two tiles of 16, each within one block.
 struct Keys {
   uint4 k[2][2];  // [tile][piece]
@@ -128,11 +128,11 @@ __device__ __forceinline__ bool deal(const AttendArgs &a, int wg, bool publish, 
 }
 
 // HW: heads side by side (their rows of a slot are neighbours in memory: 512 bytes at a time come faster than 128), one or more waves to
-// each, which take steps of 32 keys in turn.  DT: type of q and out.
+// each, which take steps of 32 keys in turn.  RT: tiles of 16 query rows, which share the keys' and values' conversion.  DT: type of q and out.
 // Accuracy: stored keys and values are bf16 numbers.  bf16 queries enter as they are; fp32 ones as three bf16 parts (24 bits).  Weights
 // enter the second product as two parts (16 bits) with bf16 outputs, three with fp32 ones.  Everything else is fp32.
-template <int DT, int HW>
-__global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_attend(AttendArgs a) {
+template <int DT, int HW, int RT>
+__global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 4) k_attend(AttendArgs a) {
   constexpr int KW = kWaves / HW;
   constexpr int NQ = DT == SKIPKV_BF16 ? 1 : 3, NP = DT == SKIPKV_BF16 ? 2 : 3;
   constexpr int ESZ = DT == SKIPKV_BF16 ? 2 : 4;
@@ -226,13 +226,14 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
   uint32_t ke = kexp[id], ve = value_scale(0);
 
   // ---- queries: lane (g, c) holds dimensions 64 i + 16 g + 8 half + (0 .. 7) of row c
-  bf16x8 qf[NQ][4];
-  int sees = 0x7FFFFFFF;  // keys that row c sees
-  {
+  bf16x8 qf[RT][NQ][4];
+  int sees[RT];  // keys that row 16 rt + c sees
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
     const uint32_t q_sign = a.scale < 0.f ? 0x80008000u : 0u;
-    const int r = r0 + c, j = r / a.group, i = r - j * a.group;
+    const int r = r0 + 16 * rt + c, j = r / a.group, i = r - j * a.group;
     const bool in = r < r1;
-    if (in) sees = n - m + j + 1;
+    sees[rt] = in ? n - m + j + 1 : 0x7FFFFFFF;
     const char *p = static_cast<const char *>(a.q) + ((q0 + j) * a.q_stride_tok + (h * a.group + i) * a.q_stride_head + 16 * g) * ESZ;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -255,15 +256,20 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
         }
       }
 #pragma unroll
-      for (int k = 0; k < NQ; ++k) qf[k][s] = frag(w[k][0] ^ q_sign, w[k][1] ^ q_sign, w[k][2] ^ q_sign, w[k][3] ^ q_sign);
+      for (int k = 0; k < NQ; ++k) qf[rt][k][s] = frag(w[k][0] ^ q_sign, w[k][1] ^ q_sign, w[k][2] ^ q_sign, w[k][3] ^ q_sign);
     }
   }
   const int all_see = max(0, n - m + r0 / a.group + 1);  // keys below this are seen by every row
 
-  f32x4 o[8];
+  f32x4 o[RT][8];
+  float ref[RT], sum[RT];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float ref = kRefInit, sum = 0.f;
+  for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    ref[rt] = kRefInit;
+    sum[rt] = 0.f;
+  }
   // (the scale's sign has gone into the queries; not 0, so that what is not seen stays -inf)
   const float to_log2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-45f);
   int nan_from = 0x7FFFFFFF;  // first step of the wave with a NaN that only some rows see
@@ -285,7 +291,7 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
       const float vs2[2] = {scale_of_byte(__builtin_amdgcn_readlane(ve, 2 * s)), scale_of_byte(__builtin_amdgcn_readlane(ve, 2 * s + 1))};
       const bool all_seen = key0 + 32 <= min(all_see, k_end);
       // ---- logits
-      f32x4 acc[2];
+      f32x4 acc[RT][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         bf16x8 kf[4];
@@ -295,12 +301,15 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
           const uint32_t w0 = s4 & 1 ? x.z : x.x, w1 = s4 & 1 ? x.w : x.y;
           kf[s4] = frag(e4m3_to_bf16x2<false>(w0, ks2[t]), e4m3_to_bf16x2<true>(w0, ks2[t]), e4m3_to_bf16x2<false>(w1, ks2[t]), e4m3_to_bf16x2<true>(w1, ks2[t]));
         }
-        f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = NQ - 1; k >= 0; --k)
+        for (int rt = 0; rt < RT; ++rt) {
+          f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int s4 = 0; s4 < 4; ++s4) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s4], qf[k][s4], z, 0, 0, 0);
-        acc[t] = z;
+          for (int k = NQ - 1; k >= 0; --k)
+#pragma unroll
+            for (int s4 = 0; s4 < 4; ++s4) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[s4], qf[rt][k][s4], z, 0, 0, 0);
+          acc[rt][t] = z;
+        }
         __builtin_amdgcn_sched_barrier(0);  // (few registers: four waves share a SIMD)
       }
       load_k(s0, after);
@@ -317,45 +326,50 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
             if (key >= k_end) x = make_uint2(0, 0);
             v_nan |= has_nan(x.x) || has_nan(x.y);
             x = make_uint2(x.x & ~nan_bytes(x.x), x.y & ~nan_bytes(x.y));  // (see below)
-            if (key >= min(sees, k_end)) acc[t][i] = -__builtin_inff();
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              if (key >= min(sees[rt], k_end)) acc[rt][t][i] = -__builtin_inff();
           }
         if (__any(v_nan)) nan_from = min(nan_from, s0 + s);
       }
       // ---- weights
-      uint32_t pf[NP][4];
-      {
-        float top = acc[0][0];
+      uint32_t pf[RT][NP][4];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, acc[i >> 2][i & 3]);
+      for (int rt = 0; rt < RT; ++rt) {
+        float top = acc[rt][0][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, acc[rt][i >> 2][i & 3]);
         top *= to_log2;
-        if (__any(top > ref + kSlack)) {
+        if (__any(top > ref[rt] + kSlack)) {
           asm volatile("");
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float now = fmaxf(ref, top), f = __builtin_amdgcn_exp2f(ref - now);
-          ref = now;
-          sum *= f;
+          const float now = fmaxf(ref[rt], top), f = __builtin_amdgcn_exp2f(ref[rt] - now);
+          ref[rt] = now;
+          sum[rt] *= f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) o[j] *= f;
+          for (int j = 0; j < 8; ++j) o[rt][j] *= f;
         }
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(fmaf(acc[i >> 2][i & 3], to_log2, -ref));
-          sum += p[i];
+          p[i] = __builtin_amdgcn_exp2f(fmaf(acc[rt][i >> 2][i & 3], to_log2, -ref[rt]));
+          sum[rt] += p[i];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t parts[NP];
           split_bf16(p[2 * i], p[2 * i + 1], parts);
 #pragma unroll
-          for (int k = 0; k < NP; ++k) pf[k][i] = parts[k];
+          for (int k = 0; k < NP; ++k) pf[rt][k][i] = parts[k];
         }
       }
       // ---- values
       value_frags(kv, vs2, [](uint32_t w) { return w; }, [&](int j, bf16x8 vf) {
 #pragma unroll
-        for (int k = NP - 1; k >= 0; --k) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(pf[k][0], pf[k][1], pf[k][2], pf[k][3]), o[j], 0, 0, 0);
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int k = NP - 1; k >= 0; --k) o[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(pf[rt][k][0], pf[rt][k][1], pf[rt][k][2], pf[rt][k][3]), o[rt][j], 0, 0, 0);
       });
       load_v(s0, after);
       __builtin_amdgcn_sched_barrier(0);
@@ -374,57 +388,64 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 ? 2 : 4) k_atten
         kv.v[t][i] = make_uint2(0, 0);
         if (p >= 0 && p < a.n_blocks) kv.v[t][i] = *reinterpret_cast<const uint2 *>(vbase + p * a.stride_block + (int64_t)(key & bmask) * a.stride_tok + 8 * c);
       }
-    uint32_t one[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = key0 + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
-      one[i] = (key < min(sees, k_end) ? 0x3F80u : 0u) | (key + 1 < min(sees, k_end) ? 0x3F800000u : 0u);
-    }
     const float unscaled[2] = {1.f, 1.f};
-    value_frags(kv, unscaled, [](uint32_t w) { return nan_bytes(w) & 0x38383838u; /* the code of 1 */ }, [&](int j, bf16x8 vf) {
-      const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(one[0], one[1], one[2], one[3]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (z[i] > 0.f) o[j][i] = nan32();
-    });
+    for (int rt = 0; rt < RT; ++rt) {
+      uint32_t one[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+        one[i] = (key < min(sees[rt], k_end) ? 0x3F80u : 0u) | (key + 1 < min(sees[rt], k_end) ? 0x3F800000u : 0u);
+      }
+      value_frags(kv, unscaled, [](uint32_t w) { return nan_bytes(w) & 0x38383838u; /* the code of 1 */ }, [&](int j, bf16x8 vf) {
+        const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(one[0], one[1], one[2], one[3]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (z[i] > 0.f) o[rt][j][i] = nan32();
+      });
+    }
   }
   poison = __any(poison);
   if (poison && n_ok && lane == 0 && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_BLOCK_TABLE);
 
-  // ---- merge of a head's waves: lane (g, c) has row c, dimensions 32 g + 8 i + j
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-  if (g == 0) ml_part[wave_all][c] = make_float2(ref, poison ? nan32() : sum);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j4 = 0; j4 < 2; ++j4)
-      *reinterpret_cast<float4 *>(&o_part[wave_all][c][32 * g + 8 * i + 4 * j4]) = make_float4(o[4 * j4][i], o[4 * j4 + 1][i], o[4 * j4 + 2][i], o[4 * j4 + 3][i]);
-  __syncthreads();
-  const int rows = r1 - r0;
+  // ---- merge of a head's waves, 16 rows at a time: lane (g, c) has row c, dimensions 32 g + 8 i + j
   const int64_t part = a.dealt ? (int64_t)blockIdx.x : (int64_t)((b * a.n_rb + rb) * n_hg + hg) * a.n_split + split;
-  for (int item = kw * 64 + lane; item < rows * (kD / 4); item += 64 * KW) {
-    const int row = item / (kD / 4), d = 4 * (item % (kD / 4)), r = r0 + row;
-    float top = kRefInit;
 #pragma unroll
-    for (int w = 0; w < KW; ++w) top = fmaxf(top, ml_part[w * HW + hw][row].x);
-    float all = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int rt = 0; rt < RT; ++rt) {
+    if (rt > 0) __syncthreads();  // (the rows before are read)
+    sum[rt] += __shfl_xor(sum[rt], 16);
+    sum[rt] += __shfl_xor(sum[rt], 32);
+    if (g == 0) ml_part[wave_all][c] = make_float2(ref[rt], poison ? nan32() : sum[rt]);
 #pragma unroll
-    for (int w = 0; w < KW; ++w) {
-      const float2 ml = ml_part[w * HW + hw][row];
-      const float f = __builtin_amdgcn_exp2f(ml.x - top);
-      const float4 x = *reinterpret_cast<const float4 *>(&o_part[w * HW + hw][row][d]);
-      all += ml.y * f;
-      v.x += x.x * f, v.y += x.y * f, v.z += x.z * f, v.w += x.w * f;
-    }
-    if (n_chunks == 1) {
-      const int j = r / a.group;
-      store_row<DT>(a, q0 + j, h * a.group + r - j * a.group, d, v, top, all);
-    } else {
-      const int64_t at = (part * HW + hw) * a.part_rows + row;
-      *reinterpret_cast<float4 *>(a.part_o + at * kD + d) = v;
-      if (d == 0) a.part_ml[at] = make_float2(top, all);
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j4 = 0; j4 < 2; ++j4)
+        *reinterpret_cast<float4 *>(&o_part[wave_all][c][32 * g + 8 * i + 4 * j4]) = make_float4(o[rt][4 * j4][i], o[rt][4 * j4 + 1][i], o[rt][4 * j4 + 2][i], o[rt][4 * j4 + 3][i]);
+    __syncthreads();
+    const int rows = min(16, r1 - r0 - 16 * rt);  // (negative: none)
+    for (int item = kw * 64 + lane; item < rows * (kD / 4); item += 64 * KW) {
+      const int row = item / (kD / 4), d = 4 * (item % (kD / 4)), r = r0 + 16 * rt + row;
+      float top = kRefInit;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) top = fmaxf(top, ml_part[w * HW + hw][row].x);
+      float all = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float2 ml = ml_part[w * HW + hw][row];
+        const float f = __builtin_amdgcn_exp2f(ml.x - top);
+        const float4 x = *reinterpret_cast<const float4 *>(&o_part[w * HW + hw][row][d]);
+        all += ml.y * f;
+        v.x += x.x * f, v.y += x.y * f, v.z += x.z * f, v.w += x.w * f;
+      }
+      if (n_chunks == 1) {
+        const int j = r / a.group;
+        store_row<DT>(a, q0 + j, h * a.group + r - j * a.group, d, v, top, all);
+      } else {
+        const int64_t at = (part * HW + hw) * a.part_rows + 16 * rt + row;
+        *reinterpret_cast<float4 *>(a.part_o + at * kD + d) = v;
+        if (d == 0) a.part_ml[at] = make_float2(top, all);
+      }
     }
   }
 }
@@ -521,64 +542,83 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
 
 }  // namespace
 
-// How the work is laid out: heads side by side, and chunks per entry.  A workgroup's unit is one step of its 8 waves, 64 KB of codes
-// whatever their number of heads; a CU takes some 2.9 us for it when the whole chip reads (3.05 and 3.3 us where two heads' rows or one's
-// lie together), the way to the first unit and from the last costs 4 us, joining chunks a launch of 5 us.  Taken is what comes out
-// shortest if all lengths were max_len.  Measured, us, one head / four heads side by side, chunks as the rule has them:
-//   64 x 4 heads, 1152 keys 15.8 / 22.5;  50 x 8 heads, 400-830 keys 18.6 / 22.8;  1 x 8 heads, 4224 keys 11.2 / 12.3;
-//   8 x 8 heads, 32896 keys 127 / 104;  18 x 8 heads, 10 K keys 110 / 74.
+// How the work is laid out: rows per workgroup, heads side by side, and chunks per entry.  Taken is what comes out shortest if all
+// lengths were max_len, by these times (us, all of them measured when the whole chip is at work):
+//   16 or 32 rows: a workgroup's unit is one step of its 8 waves, 64 KB of codes whatever their number of heads: 2.9 where four
+//     heads' rows lie together, 3.05 and 3.3 with two and one; 2.2 and 2.4 where several blocks of 16 and 32 rows read the same codes; the
+//     way to the first unit and from the last 4; a row of partial results, written and read again, 0.0003, the launch that joins them 5;
+//   256 rows (k_attend_rows; bf16, from 33 rows on): a tile of 64 keys 0.9 to 1.8, the way to the first one 8, pieces as above.
+// Measured, us, one head / four heads side by side:
+//   64 x 4 heads, 1152 keys 15.8 / 22.5;  50 x 8 heads, 400-830 keys 18.6 / 22.8;  8 x 8 heads, 32896 keys 127 / 104;  18 x 8 heads, 10 K keys 110 / 74;
+// rows of 16 / 32 / 256:
+//   20 rows, 16 x 8 heads, 4200 keys 45 / 39 / -;  32 rows, 64 x 4 heads, 1152 keys 28 / 19 / 29;  32 rows, 16 x 8 heads, 1000 keys 12.7 / 16.2 / 20;
+//   80 rows, 4 x 8 heads, 1100 keys 11.9 / 15.4 / 17.5;  160 rows 18.6 / 16.0 / 22.9;  48 rows, 30 x 4 heads, 300-2000 keys 27.7 / 22.5 / 28.2;
+//   128 rows, 64 x 8 heads, 1152 keys 123 / 106 / 69;  64 rows, 8 x 8 heads, 32000 keys 264 / 166 / 156.
+// Without the time of partial results, which made the chunks shorter: 1 x 8 heads, 4224 keys, one token 12.2 instead of 10.8.
 void plan_attend(AttendArgs *a) {
-  a->rows = 16;
-  // Two blocks of 16 rows that read the cache one behind the other are faster than a workgroup of 256 rows where the cache is long, us, 21 to 32 rows:
-  // 8 x 8 heads, 32000 keys 123 / 141;  16 x 8 heads, 4200 keys 44 / 48;  64 x 4 heads, 1152 keys 28 / 25.  From 33 rows on it is the
-  // other way round (56 rows: 207 / 145, 65 / 52, 52 / 26).
-  const int64_t rows = (int64_t)a->max_q * a->group;
-  if (a->dtype == SKIPKV_BF16 && (rows > 32 || (rows > 16 && a->max_len <= 2048))) a->rows = 256;
-  a->n_rb = (int32_t)((rows + a->rows - 1) / a->rows);
-  a->part_rows = (int32_t)std::min<int64_t>(a->rows, rows);
-  if (a->rows > 16) {  // one workgroup per CU
-    a->hw = 1;
-    a->n_entries = (int64_t)a->batch * a->n_rb * a->n_kv_heads;
-    // Up to 128 blocks of rows are cut alike here; more are dealt out by what the sequences have, us, as cut here / dealt: 8 x 8 heads, 100-400
-    // query tokens over 2-6 K keys 215 / 180;  4 x 8 heads, 700-1500 tokens 295 / 282;  30 x 8 heads, 20-40 tokens 133 / 136;  and
-    // 32 blocks in all 23.2 / 26.4.
-    const int64_t blocks = std::min<int64_t>((int64_t)a->batch * a->n_rb, ((int64_t)a->total_q * a->group + a->rows - 1) / a->rows + a->batch) * a->n_kv_heads;
-    if (a->n_entries > 128 && a->batch <= 64 * kDealt && blocks < (1 << 22)) {  // (a grid has fewer than 2^32 threads)
-      a->chunk = a->max_len;
-      a->n_split = 1;
-      a->n_parts = kRowParts;
-      a->dealt = (int32_t)blocks + kRowParts;
-      return;
-    }
-    const int64_t want = std::max<int64_t>(1, 256 / a->n_entries);
-    a->chunk = (int32_t)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
-    a->n_split = std::max(1, (a->max_len + a->chunk - 1) / a->chunk);
-    a->n_parts = a->n_entries * a->n_split;
-    return;
-  }
+  const int64_t head_rows = (int64_t)a->max_q * a->group;
+  const bool bf16 = a->dtype == SKIPKV_BF16;
+  constexpr double kPartRow = 0.0003, kJoin = 5;
   double best = 0;
   int steps = 0;  // of a workgroup
-  for (const int hw : {4, 2, 1}) {
-    if (a->n_kv_heads % hw) continue;
-    const int unit = 32 * kWaves / hw, units = std::max(1, (a->max_len + unit - 1) / unit);
-    const int64_t entries = (int64_t)a->batch * a->n_rb * (a->n_kv_heads / hw);
-    for (int turn = 0; turn <= 4; ++turn) {  // one workgroup per entry, or as many as fill the CUs so many times
-      const int64_t want = turn == 0 ? 1 : std::min<int64_t>(units, 256 * turn / entries);
-      if (want < 1) continue;
-      const int per = (int)((units + want - 1) / want), split = (units + per - 1) / per;  // units per workgroup
-      const double turns = (double)((entries * split + 255) / 256);
-      const double us = turns * (per * (hw == 4 ? 2.9 : hw == 2 ? 3.05 : 3.3) + 4) + (split > 1 ? 5 : 0);
-      if (best == 0 || us < best) {
-        best = us;
-        a->hw = hw;
-        a->chunk = per * unit;
-        a->n_split = split;
-        a->n_entries = entries;
-        steps = per;
+  for (const int rows : {16, 32}) {
+    if (rows == 32 && (!bf16 || head_rows <= 16)) continue;
+    const int64_t n_rb = (head_rows + rows - 1) / rows;
+    if (bf16 && n_rb > 16) continue;
+    const int part_rows = (int)std::min<int64_t>(rows, head_rows);
+    for (const int hw : {4, 2, 1}) {
+      if (a->n_kv_heads % hw) continue;
+      const int unit = 32 * kWaves / hw, units = std::max(1, (a->max_len + unit - 1) / unit);
+      const int64_t entries = (int64_t)a->batch * n_rb * (a->n_kv_heads / hw);
+      const double unit_us = bf16 && n_rb > 1 ? (rows == 32 ? 2.4 : 2.2) : hw == 4 ? 2.9 : hw == 2 ? 3.05 : 3.3;
+      for (int turn = 0; turn <= 4; ++turn) {  // one workgroup per entry, or as many as fill the CUs so many times
+        const int64_t want = turn == 0 ? 1 : std::min<int64_t>(units, 256 * turn / entries);
+        if (want < 1) continue;
+        const int per = (int)((units + want - 1) / want), split = (units + per - 1) / per;  // units per workgroup
+        const double turns = (double)((entries * split + 255) / 256);
+        const double us = turns * (per * unit_us + 4) + (split > 1 ? kJoin + kPartRow * (double)(entries * split * hw * part_rows) : 0);
+        if (best == 0 || us < best) {
+          best = us;
+          a->rows = rows;
+          a->n_rb = (int32_t)n_rb;
+          a->part_rows = part_rows;
+          a->hw = hw;
+          a->chunk = per * unit;
+          a->n_split = split;
+          a->n_entries = entries;
+          steps = per;
+        }
       }
     }
   }
   a->n_parts = a->n_entries * a->n_split;
+  if (bf16 && head_rows > 32) {
+    const int64_t n_rb = (head_rows + 255) / 256, entries = (int64_t)a->batch * n_rb * a->n_kv_heads;
+    const int part_rows = (int)std::min<int64_t>(256, head_rows);
+    // Up to 128 blocks of rows are cut alike; more are dealt out by what the sequences have, us, as cut here / dealt: 8 x 8 heads, 100-400
+    // query tokens over 2-6 K keys 215 / 180;  4 x 8 heads, 700-1500 tokens 295 / 282;  30 x 8 heads, 20-40 tokens 133 / 136;  and
+    // 32 blocks in all 23.2 / 26.4.
+    const int64_t blocks = std::min<int64_t>((int64_t)a->batch * n_rb, ((int64_t)a->total_q * a->group + 255) / 256 + a->batch) * a->n_kv_heads;
+    const bool dealt = entries > 128 && a->batch <= 64 * kDealt && blocks < (1 << 22);  // (a grid has fewer than 2^32 threads)
+    const int64_t want = std::max<int64_t>(1, 256 / entries);
+    const int chunk = dealt ? a->max_len : (int)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
+    const int split = dealt ? 1 : std::max(1, (a->max_len + chunk - 1) / chunk);
+    const double once = (chunk / 64 + 1) * (0.9 + 0.9 * part_rows / 256) + 8;
+    const double us = dealt ? std::max(1., (double)blocks / 256) * once + kJoin
+                            : (double)((entries * split + 255) / 256) * once + (split > 1 ? kJoin + kPartRow * (double)(entries * split * part_rows) : 0);
+    if (best == 0 || us < best) {
+      a->rows = 256;
+      a->n_rb = (int32_t)n_rb;
+      a->part_rows = part_rows;
+      a->hw = 1;
+      a->chunk = chunk;
+      a->n_split = split;
+      a->n_entries = entries;
+      a->n_parts = dealt ? kRowParts : entries * split;
+      a->dealt = dealt ? (int32_t)blocks + kRowParts : 0;
+      return;
+    }
+  }
   // Dealing costs a workgroup 2 us before its first key and pays where lengths differ, us, as planned for equal lengths / dealt:
   //   steps  8: 16 x 8 heads, 512-4096 keys 22.6 / 23.4;  8 x 8 heads, 1-8 K 22.0 / 22.4
   //   steps 16: 16 x 8 heads, 1-8 K 39.5 / 36.1;  8 x 8 heads, 2-16 K 39.3 / 37.0;  all 4000-4500 35.3 / 36.4
@@ -591,10 +631,17 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
   const dim3 grid = a.dealt ? dim3((unsigned)a.dealt) : dim3(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
   auto go = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
-    if (a.rows > 16) (void)launch_attend_rows(a, st);
-    else if (a.hw == 4) hipLaunchKernelGGL((k_attend<DT, 4>), grid, dim3(64 * kWaves), 0, st, a);
-    else if (a.hw == 2) hipLaunchKernelGGL((k_attend<DT, 2>), grid, dim3(64 * kWaves), 0, st, a);
-    else hipLaunchKernelGGL((k_attend<DT, 1>), grid, dim3(64 * kWaves), 0, st, a);
+    auto few = [&](auto rt) {
+      constexpr int RT = decltype(rt)::value;
+      if (a.hw == 4) hipLaunchKernelGGL((k_attend<DT, 4, RT>), grid, dim3(64 * kWaves), 0, st, a);
+      else if (a.hw == 2) hipLaunchKernelGGL((k_attend<DT, 2, RT>), grid, dim3(64 * kWaves), 0, st, a);
+      else hipLaunchKernelGGL((k_attend<DT, 1, RT>), grid, dim3(64 * kWaves), 0, st, a);
+    };
+    if (a.rows == 16) few(std::integral_constant<int, 1>{});
+    else if constexpr (DT == SKIPKV_BF16) {
+      if (a.rows == 32) few(std::integral_constant<int, 2>{});
+      else (void)launch_attend_rows(a, st);
+    }
     if (a.n_split == 1) return;  // (or joined already)
     const int64_t rows = a.n_entries * a.hw * a.part_rows;
     // eight chunks of a row at a time from nine on; dealt out, a row may have more than the mean: from eight on (16 x 8 heads, 2-16 K keys: 57.0

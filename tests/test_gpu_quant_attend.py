@@ -162,7 +162,7 @@ def test_layouts_strides_and_layers(layout):
         check(out, None, q, ms, lens[layer], k, v, table, 16, layer, parts_of("bf16", 3, 4), scale=0.11)
 
 
-@pytest.mark.parametrize("m,group", [(6, 2), (24, 2), (64, 4)])
+@pytest.mark.parametrize("m,group", [(6, 2), (24, 2), (64, 4), (12, 2)])
 def test_nan_values_reach_exactly_the_queries_that_see_them(m, group):
     rng = np.random.default_rng(29)
     bs = 16

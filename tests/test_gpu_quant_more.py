@@ -191,11 +191,55 @@ def test_many_rows_dealt_out(ms, longest, width):
         check(qs.out[ms[0]:], None, q[ms[0]:], ms[1:], lens[:, 1:], *pools, table[1:], 128, 0, parts_of("bf16", max(ms), 4), heads=[5])
 
 
-def test_many_rows_with_lengths_and_blocks_that_do_not_fit():
+@pytest.mark.parametrize("heads,m,longest", [(3, 200, 9000), (1, 160, 300), (2, 900, 1500)])
+def test_few_blocks_of_many_rows(heads, m, longest):
+    """Blocks of 256 rows that are all cut alike and joined."""
+    rng = np.random.default_rng(402 + m)
+    lens = rng.integers(1, longest, (heads, 1))
+    lens[0, 0] = longest
+    k, v, table = build(rng, heads, lens[None], 32)
+    q = queries(rng, m, 4 * heads, "bf16")
+    out, lse, status = run(on_device(k, v, table), 0, q, [m], lens, "bf16")
+    assert status == 0
+    check(out, lse, q, [m], lens, k, v, table, 32, 0, parts_of("bf16", m, 4))
+    table[0, longest // 32 - 1] = -7
+    out, lse, status = run(on_device(k, v, table), 0, q, [m], lens, "bf16")
+    assert status == B.DEV_BAD_BLOCK_TABLE and bool(torch.isnan(out[-1, :4]).all())
+    out, lse, status = run(on_device(k, v, table), 0, q, [m], lens, "bf16", max_len=longest - 1)
+    assert status & B.DEV_BAD_LENGTHS and bool(torch.isnan(out[:, :4]).all()) and bool(torch.isnan(lse[:, :4]).all())
+
+
+@pytest.mark.parametrize("m,group,batch", [(200, 4, 2), (200, 4, 40), (60, 8, 2)])
+def test_nan_values_reach_exactly_the_queries_that_see_them_in_blocks_of_many_rows(m, group, batch):
+    """The blocks of rows differ in what they see, and so do the rows of one; NaN also in the middle of a cache and behind its end."""
+    rng = np.random.default_rng(403 + batch)
+    lens = rng.integers(m, 700, (1, batch))
+    lens[0, :2] = 600, 450
+    k, v, table = build(rng, 1, lens[None], 16)
+    def poke(pool, b, t, d):
+        pool.codes[0, table[b, t // 16], t % 16, 0, d] = 0xFF if d % 2 else 0x7F
+    for d in (0, 5, 64, 127):
+        poke(v, 0, 600 - 2, d)
+        poke(v, 1, 450 - 1, d)
+    poke(v, 1, 450 - m + 1, 3)                   # seen by all but the first
+    poke(v, 1, 450 - m // 2, 70)                 # by query j where 450 - m + j >= 450 - m / 2: the second half
+    poke(k, 0, 600 - 1, 9)
+    poke(v, 0, 3, 77)
+    q = queries(rng, batch * m, group, "bf16")
+    out, lse, status = run(on_device(k, v, table), 0, q, [m] * batch, lens, "bf16")
+    assert status == 0
+    check(out[:2 * m], lse[:2 * m], q[:2 * m], [m, m], lens[:, :2], k, v, table[:2], 16, 0, parts_of("bf16", m, group))
+    bad = torch.isnan(out).any(1).cpu().numpy()  # [tokens, D]
+    assert bad[:m - 2].sum() == m - 2 and bad[m - 2].sum() == 5 and bad[m - 1].all()
+    assert not bad[m].any() and bad[m + 1].sum() == 1 and bad[m + m // 2 - 1].sum() == 1 and bad[m + m // 2].sum() == 2
+    assert bad[2 * m - 1].sum() == 6 and not bad[2 * m:].any()
+
+
+@pytest.mark.parametrize("ms", [[70, 66, 80], [170, 166, 180]])
+def test_many_rows_with_lengths_and_blocks_that_do_not_fit(ms):
     rng = np.random.default_rng(401)
     lens = np.array([[700, 300, 520], [80, 310, 90]])
     k, v, table = build(rng, 2, lens[None], 16)
-    ms = [70, 66, 80]
     q = queries(rng, sum(ms), 8, "bf16")
     clean, _, _ = run(on_device(k, v, table), 0, q, ms, lens, "bf16")
     bad, t2 = lens.copy(), table.copy()
@@ -204,12 +248,12 @@ def test_many_rows_with_lengths_and_blocks_that_do_not_fit():
     out, lse, status = run(on_device(k, v, t2), 0, q, ms, bad, "bf16", max_len=700)
     assert status == B.DEV_BAD_LENGTHS | B.DEV_BAD_BLOCK_TABLE
     gone = torch.zeros(sum(ms), 8, dtype=torch.bool, device="cuda")
-    gone[:70, 4:] = True
-    gone[136:, :4] = True
+    gone[:ms[0], 4:] = True
+    gone[ms[0] + ms[1]:, :4] = True
     assert bool(torch.isnan(out[gone]).all()) and bool(torch.isnan(lse[gone]).all()) and torch.equal(out[~gone], clean[~gone])
 
 
-@pytest.mark.parametrize("m", [1, 5, 90])
+@pytest.mark.parametrize("m", [1, 5, 90, 200])
 def test_in_a_graph_with_inputs_that_change(m):
     """Store, load and attention of one step, captured once and replayed with other lengths, rows and queries; eager work of the
     same kind in between."""
@@ -277,7 +321,7 @@ def test_two_calls_at_once_on_two_streams():
     k, v, table = build(rng, 4, lens[None], 16)
     qc = on_device(k, v, table)
     cases = []
-    for dtype, m in (("bf16", 1), ("bf16", 60), ("f32", 2)):
+    for dtype, m in (("bf16", 1), ("bf16", 60), ("bf16", 200), ("bf16", 7), ("f32", 2)):
         ms, q = [m] * 6, queries(rng, 6 * m, 16, dtype)
         want, _, _ = run(qc, 0, q, ms, lens, dtype)
         out = torch.zeros_like(q)
@@ -318,7 +362,7 @@ def test_sequences_that_share_blocks():
 
 
 @pytest.mark.parametrize("byte", [0, 254, 255])
-@pytest.mark.parametrize("dtype,m,group", [("bf16", 1, 4), ("f32", 2, 2), ("bf16", 40, 2)])
+@pytest.mark.parametrize("dtype,m,group", [("bf16", 1, 4), ("f32", 2, 2), ("bf16", 40, 2), ("bf16", 12, 2), ("bf16", 200, 4)])
 def test_scales_of_blocks_without_rows_do_not_matter(dtype, m, group, byte):
     """Every block that no sequence holds has a scale byte that no store writes and NaN codes; block 0 is one of them."""
     rng = np.random.default_rng(650)
