@@ -595,17 +595,19 @@ void plan_attend(AttendArgs *a) {
   if (bf16 && head_rows > 32) {
     const int64_t n_rb = (head_rows + 255) / 256, entries = (int64_t)a->batch * n_rb * a->n_kv_heads;
     const int part_rows = (int)std::min<int64_t>(256, head_rows);
-    // Up to 128 blocks of rows are cut alike; more are dealt out by what the sequences have, us, as cut here / dealt: 8 x 8 heads, 100-400
+    // Up to 128 blocks of rows are cut alike, into pieces of less than 2048 keys; others are dealt out by what the sequences have, us, as cut here / dealt: 8 x 8 heads, 100-400
     // query tokens over 2-6 K keys 215 / 180;  4 x 8 heads, 700-1500 tokens 295 / 282;  30 x 8 heads, 20-40 tokens 133 / 136;  and
     // 32 blocks in all 23.2 / 26.4.
     const int64_t blocks = std::min<int64_t>((int64_t)a->batch * n_rb, ((int64_t)a->total_q * a->group + 255) / 256 + a->batch) * a->n_kv_heads;
-    const bool dealt = entries > 128 && a->batch <= 64 * kDealt && blocks < (1 << 22);  // (a grid has fewer than 2^32 threads)
     const int64_t want = std::max<int64_t>(1, 256 / entries);
-    const int chunk = dealt ? a->max_len : (int)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
+    int chunk = (int)std::max<int64_t>(256, ((a->max_len + want - 1) / want + 63) / 64 * 64);
+    const bool dealt = (entries > 128 || chunk >= 2048) && a->batch <= 64 * kDealt && blocks < (1 << 22);  // (a grid has fewer than 2^32 threads)
+    if (dealt) chunk = a->max_len;
     const int split = dealt ? 1 : std::max(1, (a->max_len + chunk - 1) / chunk);
-    const double once = (chunk / 64 + 1) * (0.9 + 0.9 * part_rows / 256) + 8;
-    const double us = dealt ? std::max(1., (double)blocks / 256) * once + kJoin
-                            : (double)((entries * split + 255) / 256) * once + (split > 1 ? kJoin + kPartRow * (double)(entries * split * part_rows) : 0);
+    const double tile_us = 0.9 + 0.9 * part_rows / 256, turns = (double)blocks / 256;
+    const double us = dealt ? std::max(0.125, turns) * (a->max_len / 64 + 1) * tile_us + std::max(1., turns) * 8 + kJoin + kPartRow * 256 * part_rows
+                            : (double)((entries * split + 255) / 256) * ((chunk / 64 + 1) * tile_us + 8) +
+                                  (split > 1 ? kJoin + kPartRow * (double)(entries * split * part_rows) : 0);
     if (best == 0 || us < best) {
       a->rows = 256;
       a->n_rb = (int32_t)n_rb;
@@ -623,7 +625,8 @@ void plan_attend(AttendArgs *a) {
   //   steps  8: 16 x 8 heads, 512-4096 keys 22.6 / 23.4;  8 x 8 heads, 1-8 K 22.0 / 22.4
   //   steps 16: 16 x 8 heads, 1-8 K 39.5 / 36.1;  8 x 8 heads, 2-16 K 39.3 / 37.0;  all 4000-4500 35.3 / 36.4
   //   steps 32 and more: 16 x 8 heads, 2-16 K 65.2 / 57.0;  60 x 4 heads, 2-16 K 122 / 105;  all 32896 103.9 / 106.2
-  if (a->n_split > 1 && steps >= 12 && a->batch > 1 && a->n_rb == 1 && a->n_entries <= 64 * kDealt)
+  // It also pays where max_len is the room that a sequence has rather than its length, one sequence's too.
+  if (a->n_split > 1 && steps >= 12 && a->n_rb == 1 && a->n_entries <= 64 * kDealt)
     a->dealt = (int32_t)(a->n_parts = (a->n_parts + 255) / 256 * 256);
 }
 

@@ -315,6 +315,18 @@ def test_in_a_graph_with_inputs_that_change(m):
         assert bool(torch.isfinite(out).all()) and float(out.abs().max()) > 0
 
 
+@pytest.mark.parametrize("batch,m,room", [(1, 1, 8192), (1, 8, 8192), (1, 300, 2048), (3, 100, 2048), (2, 1, 4096)])
+def test_room_for_far_more_than_there_is(batch, m, room):
+    """max_len is what a table row can hold, as a captured call has it; the lengths are a small part of it."""
+    rng = np.random.default_rng(550 + batch)
+    lens = rng.integers(m, 1200, (4, batch))
+    k, v, table = build(rng, 4, lens[None], 16, width=room)
+    q = queries(rng, batch * m, 16, "bf16")
+    out, lse, status = run(on_device(k, v, table), 0, q, [m] * batch, lens, "bf16", max_len=16 * room)
+    assert status == 0
+    check(out, lse, q, [m] * batch, lens, k, v, table, 16, 0, parts_of("bf16", m, 4))
+
+
 def test_two_calls_at_once_on_two_streams():
     rng = np.random.default_rng(600)
     lens = rng.integers(1, 3000, (4, 6))
