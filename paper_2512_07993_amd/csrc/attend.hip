@@ -632,6 +632,7 @@ void plan_attend(AttendArgs *a) {
 
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
   const dim3 grid = a.dealt ? dim3((unsigned)a.dealt) : dim3(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
+  hipError_t err = hipSuccess;
   auto go = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;
     auto few = [&](auto rt) {
@@ -643,18 +644,20 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
     if (a.rows == 16) few(std::integral_constant<int, 1>{});
     else if constexpr (DT == SKIPKV_BF16) {
       if (a.rows == 32) few(std::integral_constant<int, 2>{});
-      else (void)launch_attend_rows(a, st);
+      else err = launch_attend_rows(a, st);
     }
-    if (a.n_split == 1) return;  // (or joined already)
+    if (err == hipSuccess) err = hipGetLastError();  // (asking for an error takes it away)
+    if (a.n_split == 1 || err != hipSuccess) return;  // (or joined already)
     const int64_t rows = a.n_entries * a.hw * a.part_rows;
     // eight chunks of a row at a time from nine on; dealt out, a row may have more than the mean: from eight on (16 x 8 heads, 2-16 K keys: 57.0
     // us instead of 59.0; four on average, 32 x 8 heads, 1-8 K: 66.4 instead of 64.4)
     if (a.dealt ? a.n_parts >= 8 * a.n_entries : a.n_split > 8) hipLaunchKernelGGL((k_attend_join<DT, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_attend_join<DT, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a);
+    err = hipGetLastError();
   };
   if (a.dtype == SKIPKV_F32) go(std::integral_constant<int, SKIPKV_F32>{});
   else go(std::integral_constant<int, SKIPKV_BF16>{});
-  return hipGetLastError();
+  return err;
 }
 
 }  // namespace skipkv

@@ -483,7 +483,9 @@ __global__ void __launch_bounds__(256) k_attend_join_rows(AttendArgs a) {
 hipError_t launch_attend_rows(const AttendArgs &a, hipStream_t st) {
   const dim3 grid = a.dealt ? dim3((unsigned)a.dealt) : dim3(a.n_split * a.n_kv_heads, a.n_rb, a.batch);
   hipLaunchKernelGGL(k_attend_rows, grid, dim3(64 * kRowWaves), 0, st, a);
-  if (a.dealt) hipLaunchKernelGGL(k_attend_join_rows, dim3(1024), dim3(256), 0, st, a);
+  const hipError_t err = hipGetLastError();
+  if (!a.dealt || err != hipSuccess) return err;
+  hipLaunchKernelGGL(k_attend_join_rows, dim3(1024), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -1,0 +1,118 @@
+"""What the host side of the 8-bit cache, its attention and the block tables promises beyond what it refuses: a launch that
+fails is reported.  No GPU is used."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2512_07993_amd import binding as B
+
+from test_quant_refusals import _pages, _quant, _queries, _rows
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(B._LIB_PATH):
+        from paper_2512_07993_amd.build import build_library
+        build_library()
+    yield
+
+
+# ---- launches that fail -------------------------------------------------------------------------------------
+# Stands in front of the runtime in a child process: no kernel is launched, the launch named by fail_at fails, and the last error is kept
+# until it is asked for, as the runtime keeps it.
+RUNTIME = r"""
+#include <cstddef>
+namespace { int count, at = -1, last; struct { unsigned g[3], b[3]; size_t lds; void *st; } conf; }
+struct Dim { unsigned x, y, z; };
+extern "C" {
+void fail_at(int n) { count = 0, at = n, last = 0; }
+int launches() { return count; }
+int __hipPushCallConfiguration(Dim g, Dim b, size_t lds, void *st) {
+  conf = {{g.x, g.y, g.z}, {b.x, b.y, b.z}, lds, st};
+  return 0;
+}
+int __hipPopCallConfiguration(Dim *g, Dim *b, size_t *lds, void **st) {
+  *g = {conf.g[0], conf.g[1], conf.g[2]}, *b = {conf.b[0], conf.b[1], conf.b[2]}, *lds = conf.lds, *st = conf.st;
+  return 0;
+}
+int hipLaunchKernel(const void *, Dim, Dim, void **, size_t, void *) { return count++ == at ? last = 1 : 0; }
+int hipGetLastError() { const int e = last; last = 0; return e; }
+}
+"""
+
+ATTEND = {
+    "one token": dict(max_len=60),
+    "one token, cut caches": dict(max_len=64000),
+    "fp32": dict(dtype=B.F32),
+    "32 rows": dict(max_q=8, total_q=24),
+    "many rows, cut alike": dict(max_q=200, total_q=600, max_len=1500),
+    "many rows, dealt out": dict(max_q=900, total_q=2700, max_len=64000),
+}
+
+
+def _calls():
+    import ctypes as C
+    lib = B.lib()
+    qc = _quant(table_stride=4000)
+    for name, kw in ATTEND.items():
+        need = C.c_size_t(0)
+        q = _queries(**kw)
+        assert lib.skipkv_quant_attend_workspace_bytes(C.byref(qc), C.byref(q), C.byref(need)) == B.OK
+        yield name, lambda: lib.skipkv_quant_attend(C.byref(qc), 0, C.byref(q), 0xB000, None, 0x10000, need.value, None)
+    for name, call in (("store", lib.skipkv_quant_store), ("load", lib.skipkv_quant_load)):
+        yield name, lambda: call(C.byref(qc), C.byref(_rows()), 0, None, None, None, None)
+    for name, slots, new in (("pages", 0x7000, 3), ("pages without slots", None, 0)):
+        yield name, lambda: lib.skipkv_pages_update(C.byref(_pages()), 0x5000, 1, 0x6000, new, slots, None, 0x10000, 1 << 20, None)
+
+
+def _child(runtime):
+    import ctypes as C
+    rt = C.CDLL(runtime)
+    seen = {}
+    for name, call in _calls():
+        rt.fail_at(-1)
+        ok = call()
+        n = rt.launches()
+        failed = []
+        for i in range(n):
+            rt.fail_at(i)
+            failed.append([call(), rt.launches()])
+        seen[name] = [ok, n, failed]
+    print(json.dumps(seen))
+
+
+@pytest.fixture(scope="module")
+def outcomes(tmp_path_factory):
+    d = tmp_path_factory.mktemp("runtime")
+    src, so = str(d / "runtime.cpp"), str(d / "runtime.so")
+    with open(src, "w") as f:
+        f.write(RUNTIME)
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", "-o", so, src], check=True)
+    first = [so] + [x for x in os.environ.get("LD_PRELOAD", "").split(":") if x]
+    env = dict(os.environ, LD_PRELOAD=":".join(first), PYTHONPATH=os.pathsep.join([ROOT, os.path.join(ROOT, "tests")]))
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), so], cwd=ROOT, env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return json.loads(r.stdout.strip().splitlines()[-1])
+
+
+@pytest.mark.parametrize("what", list(ATTEND) + ["store", "load", "pages", "pages without slots"])
+def test_whichever_launch_fails_the_call_says_so(outcomes, what):
+    ok, n, failed = outcomes[what]
+    assert ok == B.OK and n >= 1
+    for rc, _ in failed:
+        assert rc == B.EHIP
+
+
+@pytest.mark.parametrize("what", list(ATTEND))
+def test_nothing_is_joined_when_the_first_kernel_was_not_launched(outcomes, what):
+    _, n, failed = outcomes[what]
+    assert n == (1 if what in ("one token", "32 rows") else 2) and failed[0] == [B.EHIP, 1]
+
+
+if __name__ == "__main__":
+    _child(sys.argv[1])
