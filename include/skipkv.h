@@ -525,7 +525,7 @@ typedef struct skipkv_pages {
   int32_t *free_list;   /* device [n_blocks]: a stack of free block ids, its top at n_free - 1    */
   int32_t *n_free;      /* device [1]                                                          */
   int32_t batch;        /* at most SKIPKV_MAX_PAGES_BATCH                                        */
-  int32_t table_stride;
+  int32_t table_stride; /* entries per row: from a row to the next, and all of them the row's own       */
   int32_t block_size;   /* token slots per block, >= 1                                          */
   int32_t n_blocks;
 } skipkv_pages;
@@ -584,7 +584,7 @@ typedef struct skipkv_quant_cache {
   int32_t batch;         /* at most 65535                                                      */
   int32_t block_size;    /* 16, 32, 64 or 128                                                  */
   int32_t n_blocks;
-  int32_t table_stride;
+  int32_t table_stride;  /* entries per row: from a row to the next, and all of them may be read      */
   const int32_t *block_table; /* device [batch, table_stride]                                   */
 } skipkv_quant_cache;
 

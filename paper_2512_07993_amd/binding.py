@@ -511,8 +511,8 @@ def skipkv_step_ranges_paged(cache: PagedCache, ranges: Ranges, params: Params, 
 
 @dataclass
 class Pages:
-    """Python mirror of skipkv_pages: block_table [B, table_stride], n_held [B], free_list [n_blocks] and
-    n_free [1], int32 device tensors that skipkv_pages_update changes in place."""
+    """Python mirror of skipkv_pages: block_table [B, table_stride] (rows as far apart as they are wide), n_held [B],
+    free_list [n_blocks] and n_free [1], int32 device tensors that skipkv_pages_update changes in place."""
     block_table: torch.Tensor
     n_held: torch.Tensor
     free_list: torch.Tensor
@@ -521,10 +521,11 @@ class Pages:
 
     def c(self) -> CPages:
         bt, device = self.block_table, self.block_table.get_device()
-        assert bt.dim() == 2 and bt.shape[0] == self.n_held.numel() and (bt.stride(1) == 1 or bt.shape[1] <= 1)
+        # (the library takes a row's width for its pitch too: a view of some columns of a wider table would have it read and write the others)
+        assert bt.dim() == 2 and bt.shape[0] == self.n_held.numel() and bt.is_contiguous(), "a block table's rows have to lie as far apart as they are wide"
         assert bt.dtype == torch.int32 and self.n_free.numel() >= 1
         return CPages(bt.data_ptr(), _ints(self.n_held, device), _ints(self.free_list, device), _ints(self.n_free, device),
-                      bt.shape[0], bt.stride(0), self.block_size, self.free_list.numel())
+                      bt.shape[0], bt.shape[1], self.block_size, self.free_list.numel())
 
 
 def skipkv_pages_workspace_bytes(pages: Pages) -> int:
@@ -546,7 +547,8 @@ def skipkv_pages_update(pages: Pages, len, new_off, total_new: int, slot_map, ws
 @dataclass
 class QuantCache:
     """Python mirror of skipkv_quant_cache for pools laid out [L, blocks, slots, Hk, D] (any strides with D
-    contiguous) of uint8 or float8_e4m3fn, scale bytes [L, Hk, blocks] and a block table [B, table_stride]."""
+    contiguous) of uint8 or float8_e4m3fn, scale bytes [L, Hk, blocks] and a block table [B, table_stride] (rows as far apart as
+    they are wide)."""
     k: torch.Tensor
     v: torch.Tensor
     k_exp: torch.Tensor
@@ -557,16 +559,16 @@ class QuantCache:
         # Strides and shapes once each: a look at a tensor's stride or size costs 0.2 us, and a call for one
         # token spends longer here than on the GPU (this structure 17.8 -> 9.6 us).
         k, v, ke, ve, bt = self.k, self.v, self.k_exp, self.v_exp, self.block_table
-        st, sh, bst = k.stride(), tuple(k.shape), bt.stride()
+        st, sh = k.stride(), tuple(k.shape)
         assert len(sh) == 5 and st[4] == 1 and k.element_size() == 1 and v.stride() == st and v.shape == sh and v.element_size() == 1
         L, blocks, slots, heads, dim = sh
         exps, device = (L, heads, blocks), k.get_device()
         assert v.get_device() == ke.get_device() == ve.get_device() == bt.get_device() == device
         assert ke.dtype == ve.dtype == torch.uint8 and ke.is_contiguous() and ve.is_contiguous() and ke.shape == exps and ve.shape == exps
         batch, wide = bt.shape
-        assert bt.dtype == torch.int32 and (bst[1] == 1 or wide <= 1)
+        assert bt.dtype == torch.int32 and bt.is_contiguous(), "a block table's rows have to lie as far apart as they are wide"
         return CQuantCache(k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), st[0], st[3], st[1], st[2], L, heads, dim,
-                           batch, slots, blocks, bst[0], bt.data_ptr())
+                           batch, slots, blocks, wide, bt.data_ptr())
 
 
 @dataclass

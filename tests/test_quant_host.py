@@ -1,11 +1,12 @@
-"""What the host side of the 8-bit cache, its attention and the block tables promises beyond what it refuses: a launch that
-fails is reported.  No GPU is used."""
+"""What the host side of the 8-bit cache, its attention and the block tables promises: a launch that fails is reported, and block
+tables are as wide as their rows lie apart.  No GPU is used."""
 import json
 import os
 import subprocess
 import sys
 
 import pytest
+import torch
 
 from paper_2512_07993_amd import binding as B
 
@@ -112,6 +113,43 @@ def test_whichever_launch_fails_the_call_says_so(outcomes, what):
 def test_nothing_is_joined_when_the_first_kernel_was_not_launched(outcomes, what):
     _, n, failed = outcomes[what]
     assert n == (1 if what in ("one token", "32 rows") else 2) and failed[0] == [B.EHIP, 1]
+
+
+# ---- block tables of the binding: table_stride is a row's pitch and its width --------------------------------
+
+def _both(table):
+    """The structures of the two kinds of callers over one block table [B, entries]."""
+    z = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype)
+    batch = table.shape[0]
+    pool = lambda: z(1, 20, 16, 2, 128, dtype=torch.uint8)
+    return [lambda: B.Pages(table, z(batch), z(20), z(1), 16).c(),
+            lambda: B.QuantCache(pool(), pool(), z(1, 2, 20, dtype=torch.uint8), z(1, 2, 20, dtype=torch.uint8), table).c()]
+
+
+BIG = torch.arange(32, dtype=torch.int32).view(4, 8)
+
+
+@pytest.mark.parametrize("table", [BIG[:, :6], BIG[:, 3:], BIG[:, 3:6], BIG[::2], BIG[:, :1], BIG[1:2].expand(3, 8), BIG[:, ::2], BIG.t(),
+                                   BIG.view(2, 16)[:, :8], BIG.long()],
+                         ids=["left", "right", "middle", "every other row", "one column", "one row for all", "every other column", "transposed",
+                              "half", "64-bit"])
+def test_tables_whose_rows_lie_further_apart_than_they_are_wide_are_refused(table):
+    """The library would take the entries behind a row for the row's own, and in the last one read and write beyond the storage."""
+    for call in _both(table):
+        with pytest.raises(AssertionError):
+            call()
+
+
+@pytest.mark.parametrize("table", [BIG, BIG[1:3], BIG[2:3], BIG[3:4, 2:7], torch.arange(9, dtype=torch.int32).view(9, 1).t(),
+                                   BIG.view(-1)[5:].as_strided((1, 12), (3, 1)), torch.zeros(5, 1, dtype=torch.int32), BIG[1:2].expand(1, 8),
+                                   torch.zeros(3, 0, dtype=torch.int32), BIG[:, 2:2]],
+                         ids=["all", "some rows", "one row", "a piece of one row", "column of 9 as a row", "row of any pitch", "one column", "one row, expanded",
+                              "nothing", "nothing of a table"])
+def test_tables_are_as_wide_as_their_shape_says(table):
+    for call in _both(table):
+        c = call()
+        assert c.batch == table.shape[0] and c.table_stride == table.shape[1]
+        assert (c.block_table or 0) == table.data_ptr()
 
 
 if __name__ == "__main__":
