@@ -644,7 +644,8 @@ typedef struct skipkv_queries {
  * that descend make the sequences longer than total_q in all, may the last ones.
  * dev_status  device int32, OR-ed into; may be NULL.
  * ws    device scratch of at least skipkv_quant_attend_workspace_bytes (0 is possible: then ws may be
- *       NULL), 256-byte aligned.
+ *       NULL), 256-byte aligned.  The size never falls as batch, total_q, max_q, max_len or table_stride grow: one of the largest
+ *       call serves all smaller ones of the same heads and dtype (at most 69 MB).
  */
 int skipkv_quant_attend_workspace_bytes(const skipkv_quant_cache *qc, const skipkv_queries *queries, size_t *out_bytes);
 int skipkv_quant_attend(const skipkv_quant_cache *qc, int32_t layer, const skipkv_queries *queries, const int32_t *len,

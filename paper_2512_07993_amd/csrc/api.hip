@@ -1399,11 +1399,12 @@ int resolve_attend(const skipkv_quant_cache *qc, const skipkv_queries *qs, Atten
     // workgroups of a launch (with rows of partial results, one of the join per row at most)
     const double parts = (double)a.n_entries * a.hw * a.part_rows;
     if (a.n_rb > 65535 || (double)a.n_split * a.n_kv_heads > 2147483647.0 || (a.n_split > 1 && parts > 2147483647.0)) return SKIPKV_ECAPACITY;
-    if (a.n_split > 1 || a.dealt) {
-      const size_t rows = (size_t)a.n_parts * (size_t)a.hw * (size_t)a.part_rows;
+    // the call's own share is this or less: every plan keeps to it
+    const size_t rows = (size_t)attend_room(a);
+    if (rows > 0) {
       l.o_bytes = align_up(rows * SKIPKV_HEAD_DIM * sizeof(float));
       l.ml_bytes = align_up(rows * sizeof(float2));
-      l.total = l.o_bytes + l.ml_bytes + (a.dealt ? align_up((size_t)(2 + (a.rows == 256 ? a.batch : a.n_entries)) * 4) : 0);
+      l.total = l.o_bytes + l.ml_bytes + align_up((size_t)(2 + 64 * kDealt) * 4);
     }
   }
   *out = l;

@@ -630,6 +630,20 @@ void plan_attend(AttendArgs *a) {
     a->dealt = (int32_t)(a->n_parts = (a->n_parts + 255) / 256 * 256);
 }
 
+// Rows of partial results for which a call and every smaller one (fewer sequences, query tokens or keys, the heads alike) have room: the
+// most that plan_attend makes of them.  Its choices rise and fall with the sizes (one token of 8 heads: 1.06 MB at 32 K keys, 2.08 at
+// some shorter ones), and a workspace of the largest call has to serve the others.
+//   16 or 32 rows at a time: keys that are cut make at most four turns of 256 workgroups, dealt out or not, of hw heads' rows each;
+//   256 rows at a time: at most kRowParts pieces dealt out, 256 cut alike.
+int64_t attend_room(const AttendArgs &a) {
+  const int64_t head_rows = (int64_t)a.max_q * a.group;
+  const bool bf16 = a.dtype == SKIPKV_BF16;
+  const int hw = a.n_kv_heads % 4 == 0 ? 4 : a.n_kv_heads % 2 == 0 ? 2 : 1;
+  const int64_t few = a.max_len > 32 * kWaves / hw ? 256 * 4 * hw * std::min<int64_t>(bf16 ? 32 : 16, head_rows) : 0;  // (else one unit, which is not cut)
+  const int64_t many = bf16 && head_rows > 32 ? kRowParts * std::min<int64_t>(256, head_rows) : 0;
+  return std::max(few, many);
+}
+
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st) {
   const dim3 grid = a.dealt ? dim3((unsigned)a.dealt) : dim3(a.n_split * (a.n_kv_heads / a.hw), a.n_rb, a.batch);
   hipError_t err = hipSuccess;

@@ -382,6 +382,7 @@ struct AttendArgs {
 constexpr int kDealt = 4;         // entries (sequences) per lane where the work is dealt out by the lengths
 constexpr int kRowParts = 512;    // partial results of blocks of 256 rows
 void plan_attend(AttendArgs *a);
+int64_t attend_room(const AttendArgs &a);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t st);
 hipError_t launch_attend_rows(const AttendArgs &a, hipStream_t st);
 

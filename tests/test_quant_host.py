@@ -1,7 +1,9 @@
-"""What the host side of the 8-bit cache, its attention and the block tables promises: a launch that fails is reported, and block
-tables are as wide as their rows lie apart.  No GPU is used."""
+"""What the host side of the 8-bit cache, its attention and the block tables promises: a launch that fails is reported, block
+tables are as wide as their rows lie apart, and a workspace that serves a call serves every smaller one.  No GPU is used."""
+import ctypes as C
 import json
 import os
+import random
 import subprocess
 import sys
 
@@ -57,7 +59,6 @@ ATTEND = {
 
 
 def _calls():
-    import ctypes as C
     lib = B.lib()
     qc = _quant(table_stride=4000)
     for name, kw in ATTEND.items():
@@ -72,7 +73,6 @@ def _calls():
 
 
 def _child(runtime):
-    import ctypes as C
     rt = C.CDLL(runtime)
     seen = {}
     for name, call in _calls():
@@ -150,6 +150,48 @@ def test_tables_are_as_wide_as_their_shape_says(table):
         c = call()
         assert c.batch == table.shape[0] and c.table_stride == table.shape[1]
         assert (c.block_table or 0) == table.data_ptr()
+
+
+# ---- workspaces --------------------------------------------------------------------------------------------
+
+def _need(batch, max_q, total_q, max_len, hk=8, group=4, dtype=B.BF16, slots=64000):
+    qc = _quant(batch=batch, n_kv_heads=hk, stride_tok=hk * 128, stride_block=16 * hk * 128, table_stride=slots // 16)
+    q = _queries(dtype=dtype, n_q_heads=hk * group, q_stride_tok=hk * group * 128, out_stride_tok=hk * group * 128, max_q=max_q, total_q=total_q,
+                 max_len=max_len)
+    out = C.c_size_t(0)
+    assert B.lib().skipkv_quant_attend_workspace_bytes(C.byref(qc), C.byref(q), C.byref(out)) == B.OK
+    return out.value
+
+
+def test_one_token_over_shorter_caches_needs_no_more():
+    top = _need(1, 1, 1, 32768)
+    assert all(_need(1, 1, 1, n) <= top for n in range(64, 32768, 64))
+
+
+@pytest.mark.parametrize("dtype", [B.BF16, B.F32])
+def test_fewer_tokens_and_fewer_sequences_need_no_more(dtype):
+    need = [_need(16, m, 16 * m, 8192, dtype=dtype) for m in range(1, 300)]
+    assert need == sorted(need)
+    need = [_need(b, 1, b, 16384, dtype=dtype) for b in range(1, 300)]
+    assert need == sorted(need)
+
+
+@pytest.mark.parametrize("dtype", [B.BF16, B.F32])
+@pytest.mark.parametrize("hk,group", [(8, 4), (1, 1), (2, 7), (3, 5), (4, 8), (16, 2)])
+def test_a_workspace_serves_every_smaller_call(hk, group, dtype):
+    """One that shrinks in its sequences, its tokens, its longest query or cache, or in the room of a table row."""
+    rng = random.Random(hk * 100 + group)
+    log = lambda lo, hi: min(hi, int(lo * (hi / lo) ** rng.random() + 0.5))
+    for _ in range(1500):
+        big = [log(1, 600), log(1, 1500), 0, log(1, 64000), 16 * log(1, 4000)]
+        big[2] = rng.choice([big[0] * big[1], log(1, big[0] * big[1])])
+        small = [log(1, x) if rng.random() < 0.6 else x for x in big[:4]] + [16 * log(1, big[4] // 16)]
+        a, b = ([_need(*x[:4], hk=hk, group=group, dtype=dtype, slots=x[4])] for x in (big, small))
+        assert b <= a, (big, small)
+
+
+def test_short_caches_need_none():
+    assert _need(64, 1, 64, 64) == 0
 
 
 if __name__ == "__main__":
