@@ -549,7 +549,8 @@ typedef struct skipkv_pages {
  * slot_map  device out [n_rows, total_new] int32, or NULL.
  * A negative length or count leaves that sequence as it is (SKIPKV_DEV_BAD_LENGTHS, slots -1); n_held or n_free out
  * of range, or more blocks given back than the stack has room for, leave everything as it is
- * (SKIPKV_DEV_BAD_BLOCK_TABLE, all slots -1).
+ * (SKIPKV_DEV_BAD_BLOCK_TABLE, all slots -1).  A block id outside [0, n_blocks) is given back and taken like any other; its slots
+ * are -1, and where it is moved or a new token's position lies in it the same bit is set.
  * dev_status  device int32, OR-ed into; may be NULL.
  * ws        device scratch of at least skipkv_pages_workspace_bytes, 256-byte aligned.
  */

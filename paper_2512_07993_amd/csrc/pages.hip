@@ -156,14 +156,21 @@ __global__ void __launch_bounds__(256) k_pages_move(PagesArgs a) {
     if (tid == 0) *a.n_free = left;
     if (a.dev_status && (short_row || (tid == 0 && total.y > taken))) atomicOr(a.dev_status, SKIPKV_DEV_OUT_OF_BLOCKS);
   }
+  // (an id that does not exist is moved like any other, and reported)
+  bool no_block = false;
+  auto moved = [&](int32_t id) {
+    no_block |= (uint32_t)id >= (uint32_t)a.n_blocks;
+    return id;
+  };
   // ---- blocks of the sequences that grow (entries behind n_held), a wave to each
   for (int b = wg * 4 + (tid >> 6); b < n; b += n_wg * 4) {
     const int held = s_held[b], now = held_after(b);
-    for (int i = held + (tid & 63); i < now; i += 64) a.block_table[(int64_t)b * a.table_stride + i] = grown_at(b, i);
+    for (int i = held + (tid & 63); i < now; i += 64) a.block_table[(int64_t)b * a.table_stride + i] = moved(grown_at(b, i));
     if ((tid & 63) == 0 && now != held) a.n_held[b] = now;
   }
   // ---- what stays on the stack of the blocks given back
-  for (int i = free0 + wg * 256 + tid; i < left; i += n_wg * 256) a.free_list[i] = at(i);
+  for (int i = free0 + wg * 256 + tid; i < left; i += n_wg * 256) a.free_list[i] = moved(at(i));
+  if (no_block && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_BLOCK_TABLE);
 }
 
 // Slots of the new tokens, from the tables as they are now.  grid = (tokens / 256, rows / rows_per_wg): a thread has one token in
@@ -198,6 +205,7 @@ __global__ void __launch_bounds__(256) k_pages_slots(PagesArgs a, int rows_per_w
   const int32_t *row = a.block_table + (int64_t)l * a.table_stride;
   // eight rows at a time: their lengths, then their entries of the table, then the slots, so that the loads overlap
   constexpr int kRows = 8;
+  bool no_block = false;
   const int r1 = min((int)(blockIdx.y + 1) * rows_per_wg, a.n_rows);
   for (int r0 = blockIdx.y * rows_per_wg; r0 < r1; r0 += kRows) {
     uint32_t pos[kRows], bi[kRows];
@@ -215,9 +223,12 @@ __global__ void __launch_bounds__(256) k_pages_slots(PagesArgs a, int rows_per_w
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       const uint32_t slot = (uint32_t)id[i] * (uint32_t)a.block_size + (pos[i] - bi[i] * (uint32_t)a.block_size);
-      if (r0 + i < r1) (a.slot_map + (int64_t)(r0 + i) * a.total_new)[tok] = bi[i] < (uint32_t)held ? (int32_t)slot : -1;
+      const bool exists = (uint32_t)id[i] < (uint32_t)a.n_blocks;
+      no_block |= !exists;  // (0 where the sequence holds none, and the last row again)
+      if (r0 + i < r1) (a.slot_map + (int64_t)(r0 + i) * a.total_new)[tok] = bi[i] < (uint32_t)held && exists ? (int32_t)slot : -1;
     }
   }
+  if (no_block && a.dev_status) atomicOr(a.dev_status, SKIPKV_DEV_BAD_BLOCK_TABLE);
 }
 
 }  // namespace
