@@ -96,7 +96,8 @@ __device__ __forceinline__ bool deal_rows(const AttendArgs &a, int wg, bool publ
   *deal = RowDeal{blocks, whole, pieces};
   if (publish) {
     int first = upto - cnt;
-    if (lane == 0) a.deal[0] = whole, a.deal[1] = pieces;
+    // (offsets that descend can make more blocks than the call has workgroups: nothing is joined of pieces that nobody forms)
+    if (lane == 0) a.deal[0] = whole, a.deal[1] = whole + rest * pieces <= (int)gridDim.x ? pieces : 1;
 #pragma unroll
     for (int i = 0; i < kDealt; ++i)
       if (i < per && lane * per + i < a.batch) a.deal[2 + lane * per + i] = (first += u[i]);
