@@ -6,8 +6,8 @@ import torch
 
 from paper_2512_07993_amd import binding as B
 
-from quant_helpers import Pool, on_device
-from test_gpu_quant_attend import SCALE, _cuda, check, parts_of, queries
+from quant_helpers import Pool, attend_reference, check_close, on_device
+from test_gpu_quant_attend import SCALE, TWO_PARTS, _cuda, build, check, parts_of, queries, run
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +42,61 @@ def test_rows_beyond_the_call_are_left_alone(fill):
             check(out[m:], lse[m:], q[m:], [m], lens[:, :1], *pools, table[:1], 128, 0, parts_of("bf16", m, group), heads=[h])
         else:
             assert bool((lse[m:, group * h:group * (h + 1)] == 99).all())
+
+
+# ---- two parts of a weight ----------------------------------------------------------------------------------
+# Values of one sign: sum_t p_t |v_t| is the output itself, so the bound of two-part weights, 2^-16 of it, is small against a step of the
+# output, and the output has to be the exact one rounded, but where that lies within the bound of a border.  (The roundings of one-part
+# weights, up to 2^-8 of each, move a result of a few large weights by up to a step.)
+
+def _half_step(x):
+    return 2.0 ** (np.floor(np.log2(np.maximum(x, 2.0 ** -120))) - 8)      # bf16: 8 significant bits
+
+
+def check_rounded_once(out, q, ms, lens, k, v, table, bs, heads, scale=SCALE):
+    hk, g = lens.shape[0], q.shape[1] // lens.shape[0]
+    qn, got = q.double().cpu().numpy(), out.double().cpu().numpy()
+    at = 0
+    for b, m in enumerate(ms):
+        for h in heads:
+            n = int(lens[h, b])
+            ref, _, tol, _ = attend_reference(qn[at:at + m, h * g:(h + 1) * g], k.rows(0, h, table[b], bs, n), v.rows(0, h, table[b], bs, n), m,
+                                              scale, TWO_PARTS, device=q.device)
+            check_close(got[at:at + m, h * g:(h + 1) * g], ref, tol + _half_step(ref + tol), "sequence %d head %d: %d keys, %d queries" % (b, h, n, m))
+        at += m
+
+
+def positive(rng, heads, lens, bs):
+    k, v, table = build(rng, heads, lens[None], bs)
+    v.codes[:] = np.where((v.codes & 0x7F) == 0x7F, v.codes, v.codes & 0x7F)
+    return k, v, table
+
+
+def sharp(rng, total, heads, dtype="bf16"):
+    """Queries whose weights lie on a few keys."""
+    return queries(rng, total, heads, dtype) * 3
+
+
+@pytest.mark.parametrize("longest", [60, 700, 5000, 20000])
+@pytest.mark.parametrize("m,group", [(1, 1), (1, 4), (2, 8), (16, 1), (17, 1), (5, 4), (3, 7), (8, 4), (4, 8), (32, 1)])
+def test_up_to_32_rows_take_the_weights_in_two_parts(m, group, longest):
+    rng = np.random.default_rng(m * 10 + group)
+    lens = np.array([[longest, max(m, longest // 7)]]).repeat(2, 0)
+    lens[1] = np.maximum(m, lens[1] // 2)
+    k, v, table = positive(rng, 2, lens, 64)
+    q = sharp(rng, 2 * m, 2 * group)
+    out, _, status = run(on_device(k, v, table), 0, q, [m, m], lens, "bf16")
+    assert status == 0
+    check_rounded_once(out, q, [m, m], lens, k, v, table, 64, [0, 1])
+
+
+@pytest.mark.parametrize("batch,m,group", [(4, 20, 4), (4, 40, 4), (2, 9, 4)])
+def test_more_rows_that_are_taken_16_or_32_at_a_time_too(batch, m, group):
+    """Few sequences with so few rows that blocks of 256 would leave most CUs without work."""
+    rng = np.random.default_rng(m)
+    lens = np.full((8, batch), 1100) - np.arange(8)[:, None]
+    k, v, table = positive(rng, 8, lens, 64)
+    q = sharp(rng, batch * m, 8 * group)
+    out, _, status = run(on_device(k, v, table), 0, q, [m] * batch, lens, "bf16")
+    assert status == 0
+    check_rounded_once(out, q, [m] * batch, lens, k, v, table, 64, [0, 5])
