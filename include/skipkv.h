@@ -600,7 +600,8 @@ typedef struct skipkv_quant_cache {
  * before them and end = NULL; and the cache comes back for skipkv_step_ranges with begin = NULL, end = len.
  * skipkv_quant_store: per block and head, the scale is the least 2^e (e - 127 as above) with
  *   448 * 2^e >= the largest finite magnitude stored; values are rounded to nearest, ties to even; infinities and NaN become
- *   NaN.  A block that holds positions before begin keeps its scale if that is the larger one, else those are
+ *   NaN.  Magnitudes from 248 * 2^120 on (the ends of fp32 and bf16) round to 2^128, at every scale, which is an infinity for
+ *   whoever reads it.  A block that holds positions before begin keeps its scale if that is the larger one, else those are
  *   rounded again to the new scale.  Slots at and beyond end are not written.
  * skipkv_quant_load: code * 2^(e - 127), rounded once to the dtype of rows; other rows are not written.
  * A range with begin < 0, end < begin, end > table_stride * block_size or longer than seq_off[b+1] - seq_off[b] is skipped
@@ -634,7 +635,9 @@ typedef struct skipkv_queries {
  * is at position N - m_b + j and sees keys t <= N - m_b + j; query head i uses KV head i / n:
  *   out = sum_t softmax_t(scale * q.k_t) v_t,   lse = log sum_t exp(scale * q.k_t)  (natural logarithm).
  * A query that sees no key (N < m_b: its position is negative) gets out = 0, lse = -inf.  Slots beyond N and keys that
- * a query does not see have no influence on it, whatever they hold.
+ * a query does not see have no influence on it, whatever they hold.  An infinity or NaN among the values that it sees makes that
+ * dimension of out infinite or NaN.  The sums of weights times values are formed before they are divided, with weights of up to 2^8:
+ * they hold while N * 2^8 * max |v| < 2^128.
  * len   device [n_kv_heads, batch]: this layer's lengths, the query tokens included.
  * fp32 queries enter as three bf16 parts and fp32 weights of the softmax as three, those of bf16 queries as two, or as one where a
  * KV head has more than 32 rows (max_q * n_q_heads / n_kv_heads) and these are taken 256 at a time.  But for that and the order of

@@ -32,15 +32,15 @@ struct Values {
 };
 
 // The 8 operands (tiles of dimensions { 8m + j }) that a wave's values make.
-template <class Code, class Use>
-__device__ __forceinline__ void value_frags(const Values &kv, const float (&scale)[2], Code &&code, Use &&use) {
+template <class Use>
+__device__ __forceinline__ void value_frags(const Values &kv, const float (&scale)[2], Use &&use) {
 #pragma unroll
   for (int half = 0; half < 2; ++half) {  // dimensions 8c + 4 half + (0 .. 3)
     uint32_t w[4][2];  // [pair of keys][two dimensions]: codes of both keys side by side
 #pragma unroll
     for (int pr = 0; pr < 4; ++pr) {
       const uint2 u0 = kv.v[pr >> 1][2 * (pr & 1)], u1 = kv.v[pr >> 1][2 * (pr & 1) + 1];
-      const uint32_t a0 = code(half ? u0.y : u0.x), a1 = code(half ? u1.y : u1.x);
+      const uint32_t a0 = half ? u0.y : u0.x, a1 = half ? u1.y : u1.x;
       w[pr][0] = __builtin_amdgcn_perm(a1, a0, 0x05010400u);
       w[pr][1] = __builtin_amdgcn_perm(a1, a0, 0x07030602u);
     }
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 
   }
   // (the scale's sign has gone into the queries; not 0, so that what is not seen stays -inf)
   const float to_log2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-45f);
-  int nan_from = 0x7FFFFFFF;  // first step of the wave with a NaN that only some rows see
+  int inf_from = 0x7FFFFFFF;  // first step of the wave with a NaN or an infinity that only some rows see
   for (int s0 = 0; s0 < steps; s0 += 32) {
     if (s0 > 0) {
       const int key = tile_key(s0);
@@ -316,21 +316,23 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 
       // ---- what is not seen
       if (!all_seen) {
         asm volatile("");  // (a branch: this is not worth computing for every step)
-        bool v_nan = false;
+        uint32_t over = 0;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t room = room_of(__builtin_amdgcn_readlane(ve, 2 * s + t));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int key = key0 + 16 * t + 4 * g + i;
             uint2 &x = kv.v[t][i];
             if (key >= k_end) x = make_uint2(0, 0);
-            v_nan |= has_nan(x.x) || has_nan(x.y);
-            x = make_uint2(x.x & ~nan_bytes(x.x), x.y & ~nan_bytes(x.y));  // (see below)
+            over |= over_bits(x.x, room) | over_bits(x.y, room);
+            x = make_uint2(x.x & ~infinite_bytes(x.x, room), x.y & ~infinite_bytes(x.y, room));  // (see below)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
               if (key >= min(sees[rt], k_end)) acc[rt][t][i] = -__builtin_inff();
           }
-        if (__any(v_nan)) nan_from = min(nan_from, s0 + s);
+        }
+        if (__any(over != 0)) inf_from = min(inf_from, s0 + s);
       }
       // ---- weights
       uint32_t pf[RT][NP][4];
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 
         }
       }
       // ---- values
-      value_frags(kv, vs2, [](uint32_t w) { return w; }, [&](int j, bf16x8 vf) {
+      value_frags(kv, vs2, [&](int j, bf16x8 vf) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -375,9 +377,9 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // A weight of 0 does not undo a NaN in a matrix product, so NaN have been taken out of the values of the steps that not every row sees
-  // in full; here they are counted, with weight 1 for the rows that see them.
-  for (int s = nan_from; s < steps; ++s) {
+  // A weight of 0 does not undo a NaN or an infinity in a matrix product, so these have been taken out of the values of the steps that not
+  // every row sees in full; here they are counted, with weight 1 for the rows that see them.
+  for (int s = inf_from; s < steps; ++s) {
     const int key0 = k_begin + (s * KW + kw) * 32;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -386,7 +388,11 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 
         const int key = key0 + 16 * t + 4 * g + i;
         const int p = key < k_end ? table[key >> a.block_log2] : -1;
         kv.v[t][i] = make_uint2(0, 0);
-        if (p >= 0 && p < a.n_blocks) kv.v[t][i] = *reinterpret_cast<const uint2 *>(vbase + p * a.stride_block + (int64_t)(key & bmask) * a.stride_tok + 8 * c);
+        if (p >= 0 && p < a.n_blocks) {
+          const uint2 x = *reinterpret_cast<const uint2 *>(vbase + p * a.stride_block + (int64_t)(key & bmask) * a.stride_tok + 8 * c);
+          const uint32_t room = room_of(vexp[p]);
+          kv.v[t][i] = make_uint2(infinite_bytes(x.x, room) & 0x38383838u, infinite_bytes(x.y, room) & 0x38383838u);  // the code of 1
+        }
       }
     const float unscaled[2] = {1.f, 1.f};
 #pragma unroll
@@ -397,7 +403,7 @@ __global__ void __launch_bounds__(64 * kWaves, DT == SKIPKV_F32 || RT > 1 ? 2 : 
         const int key = key0 + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
         one[i] = (key < min(sees[rt], k_end) ? 0x3F80u : 0u) | (key + 1 < min(sees[rt], k_end) ? 0x3F800000u : 0u);
       }
-      value_frags(kv, unscaled, [](uint32_t w) { return nan_bytes(w) & 0x38383838u; /* the code of 1 */ }, [&](int j, bf16x8 vf) {
+      value_frags(kv, unscaled, [&](int j, bf16x8 vf) {
         const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, frag(one[0], one[1], one[2], one[3]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i)

@@ -49,12 +49,15 @@ __device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&out)[N])
 }
 __device__ __forceinline__ bf16x8 frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d)); }
 
-// Bytes of w that are a NaN code (0x7F, 0xFF), as 0xFF.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
-  const uint32_t high = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;  // 0x7F + 1: no carry leaves a byte
+// Codes that are no finite bf16 number: NaN (0x7F, 0xFF) and, with a block's scale byte e from 247 on, what reaches 2^128 (from code 256 =
+// 0x78 on at 2^120, eight codes fewer for each further power).  room_of: what their magnitudes lack to 0x80, in every byte.
+__device__ __forceinline__ uint32_t room_of(uint32_t e) { return 0x01010101u * (e < 247u ? 1u : 8u * (e - 246u)); }
+__device__ __forceinline__ uint32_t over_bits(uint32_t w, uint32_t room) { return ((w & 0x7F7F7F7Fu) + room) & 0x80808080u; }  // (at most 0x7F + 72: no carry leaves a byte)
+// Their bytes, as 0xFF.
+__device__ __forceinline__ uint32_t infinite_bytes(uint32_t w, uint32_t room) {
+  const uint32_t high = over_bits(w, room);
   return (high << 1) - (high >> 7);
 }
-__device__ __forceinline__ bool has_nan(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0; }
 
 // Four dimensions of a finished row (d = 0: and its lse): v / all, rounded once.
 template <int DT>

@@ -130,7 +130,7 @@ __device__ __forceinline__ bool deal_rows(const AttendArgs &a, int wg, bool publ
 
 __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a) {
   __shared__ __align__(256) char tiles[3][kTileB];
-  __shared__ int nan_tile;                              // first tile with a NaN in V that only some rows see
+  __shared__ int inf_tile;                              // first tile with a NaN or an infinity in V that only some rows see
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, hi = lane >> 5, c = lane & 31;
   const int bmask = (1 << a.block_log2) - 1;
   int split, h, rb, b;
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
   const int k_begin = split * chunk, k_end = min(most, k_begin + chunk);
   const int n_tiles = (k_end - k_begin + kTile - 1) / kTile;
   const int all_see = max(0, n - m + r0 / a.group + 1);  // keys below this are seen by every row of the workgroup
-  if (tid == 0) nan_tile = 0x7FFFFFFF;
+  if (tid == 0) inf_tile = 0x7FFFFFFF;
 
   // ---- queries: lane (hi, c) holds dimensions 16 s + 8 hi + (0 .. 7) of row c
   const int w0 = r0 + 32 * wave;  // the wave's first row
@@ -222,9 +222,10 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
         vc = make_uint4(0, 0, 0, 0);
         ve = 127;
       }
-      if (has_nan(vc.x) || has_nan(vc.y) || has_nan(vc.z) || has_nan(vc.w)) {  // counted below
-        atomicMin(&nan_tile, tile);
-        vc = make_uint4(vc.x & ~nan_bytes(vc.x), vc.y & ~nan_bytes(vc.y), vc.z & ~nan_bytes(vc.z), vc.w & ~nan_bytes(vc.w));
+      const uint32_t room = room_of(ve);
+      if (over_bits(vc.x, room) | over_bits(vc.y, room) | over_bits(vc.z, room) | over_bits(vc.w, room)) {  // counted below
+        atomicMin(&inf_tile, tile);
+        vc = make_uint4(vc.x & ~infinite_bytes(vc.x, room), vc.y & ~infinite_bytes(vc.y, room), vc.z & ~infinite_bytes(vc.z, room), vc.w & ~infinite_bytes(vc.w, room));
       }
     }
     put_codes(to + s_key * kPitchK, s_j, kc, scale_of_byte(ke));
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
   look_up(0);
   fetch(0);
   look_up(1);
-  __syncthreads();  // (nan_tile)
+  __syncthreads();  // (inf_tile)
   char *here = tiles[0], *there = tiles[1], *then = tiles[2];  // buffers of this tile, the next one, the one behind it
   auto lds_of = [](const char *p) { return (LdsPtr)(uintptr_t)lds_addr(p); };
   if (n_tiles > 0) {
@@ -377,13 +378,14 @@ __global__ void __launch_bounds__(64 * kRowWaves, 2) k_attend_rows(AttendArgs a)
     for (int tile = 0; tile < n_free; ++tile) step(std::false_type{}, tile);
     for (int tile = n_free; tile < n_tiles; ++tile) step(std::true_type{}, tile);
   }
-  // ---- NaN among the values of tiles that only some rows see: counted with weight 1 for the rows that see them
+  // ---- NaN and infinities among the values of tiles that only some rows see: counted with weight 1 for the rows that see them
   __syncthreads();
-  for (int tile = nan_tile; tile < n_tiles; ++tile) {
+  for (int tile = inf_tile; tile < n_tiles; ++tile) {
     __syncthreads();
     look_up(tile);
     fetch(tile);
-    const auto ones = [&](uint32_t w) { return k_begin + tile * kTile + s_key < k_end ? nan_bytes(w) & 0x38383838u : 0u; };  // the code of 1
+    const uint32_t room = room_of(ve);
+    const auto ones = [&](uint32_t w) { return k_begin + tile * kTile + s_key < k_end ? infinite_bytes(w, room) & 0x38383838u : 0u; };  // the code of 1
     put_codes(tiles[0] + kTileV + s_key * kPitchV, s_j, make_uint4(ones(vc.x), ones(vc.y), ones(vc.z), ones(vc.w)), 1.f);
     __syncthreads();
 #pragma unroll

@@ -1,7 +1,8 @@
 // Rows of a dense cache to and from the 8-bit one: per block of tokens and head, e4m3 codes with one power-of-two scale.
 //
 // Storing a block: a = largest finite magnitude of its new rows, scale 2^e with the least e for which a <= 448 * 2^e
-// (no value is clipped, and half the range of the format is used at least), code = x * 2^-e rounded once.  A power of two costs no
+// (no value is clipped, and half the range of the format is used at least), code = x * 2^-e rounded once.  (From 248 * 2^120
+// on that is 2^128, an infinity to whoever reads it: numbers of 4 significant bits have no other neighbour there at any scale.)  A power of two costs no
 // accuracy - e4m3 has 4 significant bits at every normal magnitude - and buys exactness afterwards: codes that move between blocks with
 // a compression step are not rounded a second time, and the attention's bf16 operands are the stored values themselves.
 // A block that already holds rows keeps the larger scale; its old codes are read and written only where the new rows

@@ -100,3 +100,39 @@ def test_more_rows_that_are_taken_16_or_32_at_a_time_too(batch, m, group):
     out, _, status = run(on_device(k, v, table), 0, q, [m] * batch, lens, "bf16")
     assert status == 0
     check_rounded_once(out, q, [m] * batch, lens, k, v, table, 64, [0, 5])
+
+
+# ---- values that no bf16 number is ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,m,group,longest", [("bf16", 5, 1, 98), ("bf16", 4, 4, 5010), ("f32", 5, 2, 98), ("f32", 3, 4, 5010), ("bf16", 8, 4, 98),
+                                                   ("bf16", 30, 1, 5010), ("bf16", 70, 8, 98), ("bf16", 200, 4, 210), ("bf16", 150, 4, 9010)])
+def test_the_largest_numbers_reach_only_the_queries_that_see_them(dtype, m, group, longest):
+    """Numbers from 248 * 2^120 on are rounded to 2^128, which is an infinity in the second product: 0 times it must not reach the queries that do not
+    see it, as 0 times a NaN does not.  The last two keys are in a block of their own and hold 0 but for these dimensions."""
+    rng = np.random.default_rng(m + group)
+    big = torch.tensor([torch.finfo(torch.bfloat16).max, 249 * 2.0 ** 120, -448.0 * 2.0 ** 119, torch.finfo(torch.bfloat16).min]).double().numpy()
+    dims, bs = [0, 29, 64, 127], 16
+    lens = np.array([[longest, longest - 8]])
+    k, v, table = build(rng, 1, lens[None], bs)
+    rows = np.zeros((2, 128))
+    rows[0, dims] = big
+    rows[1, dims[0]] = big[0]
+    at = longest - 2
+    assert at % bs == 0
+    v.store(0, 0, table[0], bs, at, rows)
+    assert v.byte[0, 0, table[0, at // bs]] == 247
+    ms = [m, min(m, 3)]
+    q = queries(rng, sum(ms), group, dtype)
+    out, lse, status = run(on_device(k, v, table), 0, q, ms, lens, dtype)
+    assert status == 0
+    far = [d for d in dims if d != dims[2]]                    # (448 * 2^119 is a bf16 number, and in the sums below too large to compare)
+    assert bool(torch.isfinite(out[:m - 2]).all()) and bool(torch.isfinite(out[m:]).all())
+    assert not bool(torch.isfinite(out[m - 2:m][:, :, far]).any())
+    rest = [d for d in range(128) if d not in dims]
+    assert bool(torch.isfinite(out[:, :, rest]).all())
+    for d in dims:                                             # what the others see: as without those two
+        v.codes[0, table[0, at // bs], :2, 0, d] = 0
+    same, slse, status = run(on_device(k, v, table), 0, q, ms, lens, dtype)
+    assert status == 0 and torch.equal(lse, slse)
+    assert torch.equal(out[:m - 2], same[:m - 2]) and torch.equal(out[m:], same[m:]) and torch.equal(out[:, :, rest], same[:, :, rest])
+    check(same, slse, q, ms, lens, k, v, table, bs, 0, parts_of(dtype, m, group))
