@@ -544,6 +544,9 @@ def skipkv_pages_update(pages: Pages, len, new_off, total_new: int, slot_map, ws
                                      _ints(slot_map, device, True), _ptr(dev_status), _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+
+
 @dataclass
 class QuantCache:
     """Python mirror of skipkv_quant_cache for pools laid out [L, blocks, slots, Hk, D] (any strides with D
@@ -560,7 +563,8 @@ class QuantCache:
         # token spends longer here than on the GPU (this structure 17.8 -> 9.6 us).
         k, v, ke, ve, bt = self.k, self.v, self.k_exp, self.v_exp, self.block_table
         st, sh = k.stride(), tuple(k.shape)
-        assert len(sh) == 5 and st[4] == 1 and k.element_size() == 1 and v.stride() == st and v.shape == sh and v.element_size() == 1
+        assert len(sh) == 5 and st[4] == 1 and v.stride() == st and v.shape == sh
+        assert k.dtype in _CODES and v.dtype in _CODES, "pools hold e4m3 codes: uint8 or float8_e4m3fn"
         L, blocks, slots, heads, dim = sh
         exps, device = (L, heads, blocks), k.get_device()
         assert v.get_device() == ke.get_device() == ve.get_device() == bt.get_device() == device

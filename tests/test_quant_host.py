@@ -152,6 +152,20 @@ def test_tables_are_as_wide_as_their_shape_says(table):
         assert (c.block_table or 0) == table.data_ptr()
 
 
+# ---- pools: codes are e4m3 -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.int8, torch.bool, torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.int16, torch.bfloat16])
+def test_pools_of_another_form_are_refused(dtype):
+    z = lambda *shape, dt=torch.uint8: torch.zeros(shape, dtype=dt)
+    exp, table = z(1, 2, 20), z(3, 8, dt=torch.int32)
+    pool = (1, 20, 16, 2, 128)
+    for k, v in ((dtype, dtype), (torch.uint8, dtype), (dtype, torch.float8_e4m3fn)):
+        with pytest.raises(AssertionError):
+            B.QuantCache(z(*pool, dt=k), z(*pool, dt=v), exp, exp, table).c()
+    for good in (torch.uint8, torch.float8_e4m3fn):
+        assert B.QuantCache(z(*pool, dt=good), z(*pool, dt=good), exp, exp, table).c().n_blocks == 20
+
+
 # ---- workspaces --------------------------------------------------------------------------------------------
 
 def _need(batch, max_q, total_q, max_len, hk=8, group=4, dtype=B.BF16, slots=64000):
