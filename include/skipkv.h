@@ -642,8 +642,8 @@ typedef struct skipkv_queries {
  * fp32 queries enter as three bf16 parts and fp32 weights of the softmax as three, those of bf16 queries as two, or as one where a
  * KV head has more than 32 rows (max_q * n_q_heads / n_kv_heads) and these are taken 256 at a time.  But for that and the order of
  * additions the result does not depend on max_len and max_q.  A length that is negative, above
- * max_len or above table_stride * block_size (SKIPKV_DEV_BAD_LENGTHS), or a block id outside [0, n_blocks) among a head's
- * blocks (SKIPKV_DEV_BAD_BLOCK_TABLE), makes the rows concerned NaN; a sequence whose q_off entries
+ * max_len or above table_stride * block_size (SKIPKV_DEV_BAD_LENGTHS) makes all rows of its head and sequence NaN, a block id
+ * outside [0, n_blocks) (SKIPKV_DEV_BAD_BLOCK_TABLE) those that see keys in it and such as are worked on with them; a sequence whose q_off entries
  * descend, leave [0, total_q] or are more than max_q apart gets no output (SKIPKV_DEV_BAD_LENGTHS), nor, where entries
  * that descend make the sequences longer than total_q in all, may the last ones.
  * dev_status  device int32, OR-ed into; may be NULL.

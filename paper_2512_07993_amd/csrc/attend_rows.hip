@@ -7,15 +7,22 @@
 // weights from there as they lie: the keys of a matrix instruction are 16 k + 4 hi + (0 .. 3) and 8 further on, which transposing
 // reads of V's rows deliver in that order.
 //
-// What bounds it: the matrix pipe is busy for 47 % of the time and vector instructions are issued for 51 %; a SIMD overlaps the two up to
-// some six vector instructions per matrix instruction of 32 cycles (18.8 ns against 15.5 alone, 23 with eight), and this has 6.5: per weight
-// an fma, an exponential (two issue slots), an addition, half a conversion and half a maximum, besides the staging.  So everything but the
+// What bounds it: per matrix instruction of 32 cycles 68 pass on a SIMD, 35 of which issue vector instructions (per weight an fma, an
+// exponential of two issue slots, an addition, half a conversion and half a maximum, besides the staging: 6.6 per matrix instruction).  The
+// matrix pipe is busy for 47 % of the time and vector instructions are issued for 50 %, which is what two engines look like that take turns;
+// a wave waits 29 % of its time for LDS, memory or the barrier and 35 % for its turn to issue.  (Without memory, six independent vector
+// instructions beside each matrix instruction take 18.8 ns instead of 15.5, eight 23: this does not reach that.)  So everything but the
 // matrix instructions is dealt out evenly among them; operands are in registers a block of 32 keys ahead; rows in shared memory are
 // padded, not swizzled, so that addresses are immediates.  4 sequences of 3.5-4.3 K keys, 1.0-1.5 K query tokens, 8 x 4 heads (256 GFLOP):
-// 283 to 304 us from run to run, 840-900 TFLOP/s (a library's product of square matrices reaches 1.2-1.3 PFLOP/s); before blocks were dealt
+// 280 to 304 us from run to run, 840-915 TFLOP/s (a library's product of square matrices reaches 1.2-1.3 PFLOP/s); before blocks were dealt
 // out 294 to 316: 11 us less each time; before that, with all weights before the product and swizzled addresses 7 % more, without
 // the pipeline across blocks 15 % more.  32 x 32 tiles with 64 rows per wave need more registers than two waves on a
 // SIMD have (544 us).
+//
+// Weights enter the product with V rounded to one bf16 number (half a step, 2^-8 of each at most; their sum is of the unrounded ones).  Two
+// numbers, as with few rows, take eight more matrix instructions and some 40 vector instructions per block: 380 us instead of 280 in the case
+// above.  The error against 64 bits, of the result's norm (300 tokens over 3.5-4 K keys): 1.99e-3 instead of 1.64e-3, which rounding the
+// result to bf16 makes by itself.
 #include <algorithm>
 #include <type_traits>
 

@@ -10,9 +10,9 @@
 //
 // Three kernels: the blocks that every sequence needs, the blocks moved, the slots.  A kernel of its own for the slots reads finished
 // tables; with the slots in the second one, whose workgroups then look up each grown block in the prefix sums, a call takes 17 instead
-// of 13 us (64 sequences, one token, 112 rows) and 53 instead of 34 (256 sequences, 342 tokens each, 256 rows: 90 MB of slots).
+// of 13 us (64 sequences, one token, 112 rows) and 53 instead of 34 us (256 sequences, 342 tokens each, 256 rows: 90 MB of slots).
 // Bound by the latency of the launches and of their chains of loads (some 12 us), and by the slots' writes where there are many
-// new tokens: 21 us for the 90 MB.
+// new tokens: 22 us for the 90 MB.
 #include <algorithm>
 
 #include "common.h"
