@@ -191,6 +191,22 @@ def _ints(t, device: int, optional=False) -> Optional[int]:
     return t.data_ptr()
 
 
+def _scratch(ws, device: int):
+    """Address and bytes of a workspace without gaps that lies on `device`."""
+    if ws is None:
+        return None, 0
+    assert ws.is_contiguous() and ws.get_device() == device, "the workspace has to be contiguous, on the device of the other tensors"
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _status(t, device: int) -> Optional[int]:
+    """Address of a status word: int32, on `device` or in pinned memory."""
+    if t is None or isinstance(t, int):
+        return t
+    assert t.dtype == torch.int32 and (t.get_device() == device or t.is_pinned()), "the status word has to be int32, on the device of the other tensors"
+    return t.data_ptr()
+
+
 def _here(t) -> int:
     """Device of a tensor, which has to be the current one: a launch goes there."""
     device = t.get_device()
@@ -541,7 +557,7 @@ def skipkv_pages_update(pages: Pages, len, new_off, total_new: int, slot_map, ws
     n_rows = len.numel() // max(batch, 1) if len.numel() else 1
     assert slot_map is None or slot_map.numel() == n_rows * total_new
     _check(lib().skipkv_pages_update(C.byref(pages.c()), _ints(len, device), n_rows, _ints(new_off, device, True), total_new,
-                                     _ints(slot_map, device, True), _ptr(dev_status), _ptr(ws), _nbytes(ws), _stream(stream)))
+                                     _ints(slot_map, device, True), _status(dev_status, device), *_scratch(ws, device), _stream(stream)))
 
 
 _CODES = (torch.uint8, torch.float8_e4m3fn)
@@ -602,7 +618,7 @@ def _quant_rows(call, qc: QuantCache, rows: Cache, first_layer: int, begin, end,
     for t in (begin, end):
         assert t is None or t.numel() == rows.k.shape[0] * qc.k.shape[3] * qc.block_table.shape[0]
     _check(call(C.byref(qc.c()), C.byref(rows.c()), first_layer, _ints(begin, device, True), _ints(end, device, True),
-                _ptr(dev_status), _stream(stream)))
+                _status(dev_status, device), _stream(stream)))
 
 
 def skipkv_quant_store(qc: QuantCache, rows: Cache, first_layer: int, begin, end, dev_status=None, stream=None) -> None:
@@ -623,8 +639,8 @@ def skipkv_quant_attend(qc: QuantCache, layer: int, queries: Queries, len, ws, d
     device = _here(qc.k)
     assert len.shape == (qc.k.shape[3], qc.block_table.shape[0]) and queries.q.get_device() == device
     assert queries.q_off.numel() == len.shape[1] + 1
-    _check(lib().skipkv_quant_attend(C.byref(qc.c()), layer, C.byref(queries.c()), _ints(len, device), _ptr(dev_status), _ptr(ws),
-                                     _nbytes(ws), _stream(stream)))
+    _check(lib().skipkv_quant_attend(C.byref(qc.c()), layer, C.byref(queries.c()), _ints(len, device),
+                                     _status(dev_status, device), *_scratch(ws, device), _stream(stream)))
 
 
 def skipkv_similarity_workspace_bytes(cache: Cache, d_model: int) -> int:

@@ -6,7 +6,7 @@ import torch
 
 from paper_2512_07993_amd import binding as B
 
-from quant_helpers import Pool, attend_reference, check_close, on_device
+from quant_helpers import D, Pool, attend_reference, check_close, on_device
 from test_gpu_quant_attend import SCALE, TWO_PARTS, _cuda, build, check, parts_of, queries, run
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +136,30 @@ def test_the_largest_numbers_reach_only_the_queries_that_see_them(dtype, m, grou
     assert status == 0 and torch.equal(lse, slse)
     assert torch.equal(out[:m - 2], same[:m - 2]) and torch.equal(out[m:], same[m:]) and torch.equal(out[:, :, rest], same[:, :, rest])
     check(same, slse, q, ms, lens, k, v, table, bs, 0, parts_of(dtype, m, group))
+
+
+def test_workspaces_and_status_words_elsewhere_are_refused():
+    """In host memory, or with gaps: before anything is launched."""
+    rng = np.random.default_rng(5)
+    lens = np.array([[500, 30]])
+    k, v, table = build(rng, 1, lens[None], 16)
+    qc, q, n = on_device(k, v, table), queries(rng, 2, 4, "bf16"), _cuda(lens.astype(np.int32))
+    off = _cuda(np.array([0, 1, 2], dtype=np.int32))
+    qs = B.Queries(q, torch.zeros_like(q), off, max_q=1, max_len=500, scale=SCALE)
+    pages = B.Pages(qc.block_table, _cuda(np.array([2, 2], dtype=np.int32)), torch.zeros(9, dtype=torch.int32, device="cuda"),
+                    torch.zeros(1, dtype=torch.int32, device="cuda"), 16)
+    rows = B.Cache(*(torch.zeros((1, 1, 2, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)), 4, off, off, off, 2, 0)
+    need = B.skipkv_quant_attend_workspace_bytes(qc, qs)
+    good, status = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    calls = [lambda ws, st: B.skipkv_quant_attend(qc, 0, qs, n, ws, st), lambda ws, st: B.skipkv_pages_update(pages, n, off, 2, None, ws, st),
+             lambda ws, st: B.skipkv_quant_store(qc, rows, 0, None, None, st), lambda ws, st: B.skipkv_quant_load(qc, rows, 0, None, None, st)]
+    for call in calls[:2]:
+        for ws in (good.cpu(), torch.empty(4 * need, dtype=torch.uint8, device="cuda")[::4]):
+            with pytest.raises(AssertionError, match="workspace"):
+                call(ws, status)
+    for call in calls:
+        for st in (status.cpu(), status.long()):
+            with pytest.raises(AssertionError, match="status"):
+                call(good, st)
+    B.skipkv_quant_attend(qc, 0, qs, n, good, status)
+    assert int(status.item()) == 0 and bool(torch.isfinite(qs.out).all())

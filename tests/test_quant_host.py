@@ -166,7 +166,41 @@ def test_pools_of_another_form_are_refused(dtype):
         assert B.QuantCache(z(*pool, dt=good), z(*pool, dt=good), exp, exp, table).c().n_blocks == 20
 
 
-# ---- workspaces --------------------------------------------------------------------------------------------
+# ---- workspaces and status words ----------------------------------------------------------------------------
+
+def _entry_points():
+    """The calls of the binding that take a workspace or a status word, on host tensors: (name, call(ws, dev_status))."""
+    z = lambda *shape, dt=torch.int32: torch.zeros(shape, dtype=dt)
+    u8, bf = torch.uint8, torch.bfloat16
+    qc = B.QuantCache(z(1, 20, 16, 2, 128, dt=u8), z(1, 20, 16, 2, 128, dt=u8), z(1, 2, 20, dt=u8), z(1, 2, 20, dt=u8), z(3, 8))
+    off = torch.tensor([0, 1, 2, 3], dtype=torch.int32)
+    rows = B.Cache(z(1, 2, 3, 128, dt=bf), z(1, 2, 3, 128, dt=bf), 2, off, None, None, 3, 0)
+    qs = B.Queries(z(3, 4, 128, dt=bf), z(3, 4, 128, dt=bf), off, max_q=1, max_len=128, scale=0.1)
+    pages = B.Pages(qc.block_table, z(3), z(20), z(1), 16)
+    return {"attend": lambda ws, st: B.skipkv_quant_attend(qc, 0, qs, z(2, 3), ws, st),
+            "pages": lambda ws, st: B.skipkv_pages_update(pages, z(1, 3), off, 3, None, ws, st),
+            "store": lambda ws, st: B.skipkv_quant_store(qc, rows, 0, None, None, st),
+            "load": lambda ws, st: B.skipkv_quant_load(qc, rows, 0, None, None, st)}
+
+
+@pytest.mark.parametrize("name", ["attend", "pages"])
+def test_a_workspace_with_gaps_is_refused(name):
+    """Its size counts its elements, not the span that they lie in."""
+    call = _entry_points()[name]
+    for ws in (torch.zeros(1 << 20, dtype=torch.uint8)[::4], torch.zeros((64, 4096), dtype=torch.uint8)[:, :2048], torch.zeros(1, dtype=torch.uint8).expand(1 << 22)):
+        with pytest.raises(AssertionError, match="workspace"):
+            call(ws, None)
+
+
+@pytest.mark.parametrize("name", ["attend", "pages", "store", "load"])
+def test_a_status_word_of_another_type_is_refused(name):
+    call, ws = _entry_points()[name], torch.zeros(1 << 20, dtype=torch.uint8)
+    for status in (torch.zeros(1, dtype=torch.int64), torch.zeros(1, dtype=torch.int16), torch.zeros(1)):
+        with pytest.raises(AssertionError, match="status"):
+            call(ws, status)
+
+
+# ---- sizes of workspaces -------------------------------------------------------------------------------------
 
 def _need(batch, max_q, total_q, max_len, hk=8, group=4, dtype=B.BF16, slots=64000):
     qc = _quant(batch=batch, n_kv_heads=hk, stride_tok=hk * 128, stride_block=16 * hk * 128, table_stride=slots // 16)
