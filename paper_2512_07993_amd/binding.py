@@ -210,7 +210,10 @@ def _status(t, device: int) -> Optional[int]:
 def _here(t) -> int:
     """Device of a tensor, which has to be the current one: a launch goes there."""
     device = t.get_device()
-    assert device < 0 or device == torch._C._cuda_getDevice(), "the tensors are on another device than the current one"
+    if device < 0:  # (without a GPU the launch fails by itself)
+        assert not torch.cuda.is_available(), "the tensors are in host memory"
+    else:
+        assert device == torch._C._cuda_getDevice(), "the tensors are on another device than the current one"
     return device
 
 

@@ -7,6 +7,7 @@ import torch
 from paper_2512_07993_amd import binding as B
 
 from quant_helpers import D, Pool, attend_reference, check_close, on_device
+from test_quant_host import _entry_points
 from test_gpu_quant_attend import SCALE, TWO_PARTS, _cuda, build, check, parts_of, queries, run
 
 pytestmark = pytest.mark.gpu
@@ -163,3 +164,9 @@ def test_workspaces_and_status_words_elsewhere_are_refused():
                 call(good, st)
     B.skipkv_quant_attend(qc, 0, qs, n, good, status)
     assert int(status.item()) == 0 and bool(torch.isfinite(qs.out).all())
+
+
+@pytest.mark.parametrize("name", ["attend", "pages", "store", "load"])
+def test_calls_on_tensors_in_host_memory_are_refused(name):
+    with pytest.raises(AssertionError, match="host memory"):
+        _entry_points()[name](torch.zeros(1 << 20, dtype=torch.uint8), None)

@@ -183,6 +183,7 @@ def _entry_points():
             "load": lambda ws, st: B.skipkv_quant_load(qc, rows, 0, None, None, st)}
 
 
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="tensors in host memory are refused where there is a GPU")
 @pytest.mark.parametrize("name", ["attend", "pages"])
 def test_a_workspace_with_gaps_is_refused(name):
     """Its size counts its elements, not the span that they lie in."""
@@ -192,6 +193,7 @@ def test_a_workspace_with_gaps_is_refused(name):
             call(ws, None)
 
 
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="tensors in host memory are refused where there is a GPU")
 @pytest.mark.parametrize("name", ["attend", "pages", "store", "load"])
 def test_a_status_word_of_another_type_is_refused(name):
     call, ws = _entry_points()[name], torch.zeros(1 << 20, dtype=torch.uint8)
